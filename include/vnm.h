@@ -369,6 +369,133 @@ enum vnm_lsa_method { VNM_LSA_AUTO = 0, VNM_LSA_HUNGARIAN = 1, VNM_LSA_AUCTION =
 int vnm_lsa_max(const void* gain, int n, void* assign, int64_t* total);
 int vnm_lsa_max_method(const void* gain, int n, int method, void* assign, int64_t* total);
 
+/*
+ * ---- Layers in 8-bit integers -------------------------------------------------------------------
+ *
+ * The V:N:M layer with int8 activations (one scale per token) and int8 weights (one scale per output
+ * channel), and what stands between two such layers.  Types of floating-point tensors:
+ */
+typedef enum vnm_dtype { VNM_F16 = 0, VNM_F32 = 1, VNM_BF16 = 2 } vnm_dtype;
+
+/*
+ * Activations to int8 with one scale per token:
+ *   top[t] = max_i |X[t, i]|,  scale[t] = top[t] / 127,  Q[t, i] = rint(X[t, i] * f),  f = 127 / top[t]
+ * in fp32, both quotients correctly rounded; the product with f is rounded once, to the integer (nearest,
+ * ties to even), so that the result is defined to the bit.  |Q| <= 127.  A token whose top is below
+ * 2^-100 gets scale 0 and zeros; one that holds an infinity or a NaN gets scale NaN and zeros, and so
+ * every result that is computed from it is NaN.
+ *   X      dev [T x n] of type x_dtype (a vnm_dtype), leading dimension ldx >= n
+ *   Q      dev int8 [T x n], leading dimension ldq >= n (bytes between n and ldq are not written)
+ *   scale  dev fp32 [T]
+ * T == 0 is a successful no-op.
+ */
+int vnm_quantize_x(const void* X, int64_t T, int64_t n, int64_t ldx, int x_dtype, void* Q, int64_t ldq,
+                   void* scale, void* stream);
+
+/*
+ * The compressed weight in 8 bits: int8 values in place of the fp16 ones, meta and colidx unchanged,
+ * and fp32 scales [out].  `packed` is an opaque matrix-core copy as for the fp16 product, of
+ * vnm_i8_packed_bytes bytes (0: this V, M has none); it holds values, positions and columns.
+ *
+ * vnm_quantize_compressed: qvalues int8 [out_pad x 2*col_blocks] and scale fp32 [out] from the fp16
+ * values, each output channel as vnm_quantize_x treats a token (pad rows: zeros); fills `packed` too
+ * unless it is NULL.
+ * vnm_pack_i8: `packed` from a triple with int8 values (e.g. one loaded from storage); values at
+ * columns >= in count as 0.
+ */
+int vnm_i8_packed_bytes(int64_t out, int64_t in, int V, int N, int M, int64_t* bytes);
+int vnm_quantize_compressed(const void* values, const void* meta, const void* colidx, int64_t out, int64_t in,
+                            int V, int N, int M, void* qvalues, void* scale, void* packed, void* stream);
+int vnm_pack_i8(const void* qvalues, const void* meta, const void* colidx, int64_t out, int64_t in, int V, int N,
+                int M, void* packed, void* stream);
+
+/*
+ * The product in 8-bit integers:
+ *   a[t, o] = sum_b sum_{j<2} qvalues[o, 2b+j] * Q[t, b*M + colidx[o / V, b, pos_j(o, b)]]   (int32, exact)
+ *   Y[t, o] = ((float)a[t, o] * scale_w[o]) * scale_x[t] + bias[o]
+ * in fp32 with every operation rounded by itself, then rounded to y_dtype; all kernels give the same bits.
+ * Q counts as 0 at padded columns and is never read there.
+ *   Q        dev int8 [T x in], leading dimension ldq >= in; scale_x dev fp32 [T]; scale_w dev fp32 [out]
+ *   bias     dev fp16 [out] or NULL
+ *   Y        dev [T x out] of type y_dtype (a vnm_dtype), leading dimension ldy >= out
+ *   packed   dev, 256-byte aligned, or NULL (the kernel on the triple then serves the call)
+ *   path     a vnm_spmm_path; VNM_PATH_SMFMAC fails with UNSUPPORTED where the matrix-core kernels do not apply
+ *   workspace  dev, 256-byte aligned, vnm_spmm_i8_workspace_bytes(T, ...) bytes; contents are scratch
+ * The matrix-core kernels need V in {32, 64, 128}, M <= 16, ldq % 16 == 0 and Q 16-byte aligned (`in` is
+ * free).  Where they apply and the workspace is missing or too small the call fails with VNM_ERR_WORKSPACE.
+ * Layers whose sums could leave 32 bits (2 * col_blocks * 2^14 > 2^31 - 1) fail with VNM_ERR_UNSUPPORTED.
+ * T == 0 is a successful no-op (Q, scale_x and Y may then be NULL).
+ */
+int vnm_spmm_i8(const void* Q, int64_t T, int64_t ldq, const void* scale_x, const void* qvalues, const void* meta,
+                const void* colidx, const void* packed, const void* scale_w, int64_t out, int64_t in, int V, int N,
+                int M, const void* bias, void* Y, int64_t ldy, int y_dtype, int path, void* workspace,
+                int64_t workspace_bytes, void* stream);
+int vnm_spmm_i8_workspace_bytes(int64_t T, int64_t out, int64_t in, int V, int N, int M, int64_t* bytes);
+
+/*
+ * What stands between two blocks: the norm after a block, its gate, the residual addition, and the norm
+ * in front of the next block, in one pass over the tokens:
+ *   p[t]  = norm_post(y[t])                         the block's output, normalised unless post is VNM_NORM_NONE
+ *   h'[t] = residual_scale * h[t] + gate[g(t)] * p[t]                   the new residual stream -> h_out
+ *   x[t]  = norm_pre(h'[t])                         the next block's input -> x, or int8 -> q and q_scale
+ *   norm(v) = (v - mean) * r * weight + bias,  r = 1 / sqrt(mean((v - mean)^2) + eps)   VNM_NORM_LAYER
+ *   norm(v) = v * r * weight + bias,           r = 1 / sqrt(mean(v^2) + eps)            VNM_NORM_RMS
+ * All in fp32 from the inputs to each output's one rounding: x is computed from h' before h' is rounded
+ * to h_dtype, and the int8 result (as vnm_quantize_x defines it) from x in fp32.
+ *   T, n            tokens and channels, 1 <= n <= VNM_NORM_MAX_CHANNELS
+ *   h, h_out        dev [T x n], type h_dtype; h_out may be h itself, or NULL (not stored)
+ *   y               dev [T x n], type x_dtype, or NULL: h' = residual_scale * h (gate NULL, post NONE then)
+ *   gate            dev, type x_dtype, rows of n; g(t) = t / gate_tokens, or 0 for all t if gate_tokens is 0;
+ *                   leading dimension ldg; NULL = 1
+ *   *_weight, *_bias   dev [n], type x_dtype; NULL = 1 and 0
+ *   x               dev [T x n], type x_dtype, or NULL;  q dev int8 [T x n] with q_scale dev fp32 [T], or NULL;
+ *                   at most one of x and q, and at least one of x, q and h_out
+ *   stats           dev fp32 [T x 4] or NULL: mean and r of the post norm, mean and r of the pre norm (0 and 1
+ *                   where there is no norm; mean 0 for VNM_NORM_RMS); what the backward pass needs
+ * h_dtype is x_dtype or VNM_F32.  Leading dimensions in elements, each >= n.  eps > 0.  Outputs overlap no
+ * input other than h_out = h (same pointer, ldho = ldh).  T == 0 is a successful no-op.
+ */
+typedef enum vnm_norm { VNM_NORM_NONE = 0, VNM_NORM_RMS = 1, VNM_NORM_LAYER = 2 } vnm_norm;
+#define VNM_NORM_MAX_CHANNELS 16384
+typedef struct vnm_residual_norm_args {
+  int64_t T, n;
+  int h_dtype, x_dtype, post, pre;
+  float post_eps, pre_eps, residual_scale;
+  int64_t gate_tokens;
+  const void *h, *y, *gate, *post_weight, *post_bias, *pre_weight, *pre_bias;
+  int64_t ldh, ldy, ldg;
+  void *h_out, *x, *q, *q_scale, *stats;
+  int64_t ldho, ldx, ldq;
+} vnm_residual_norm_args;
+int vnm_residual_norm(const vnm_residual_norm_args* a, void* stream);
+
+/*
+ * The gradients of the above, from those of its outputs (int8 results have none):
+ *   dx, dh_out   gradients of x (type x_dtype) and of h' (type h_dtype); NULL = 0, not both
+ *   h_out, stats, y, gate, weights, biases   the forward pass's outputs and inputs (`h_new` = its h_out; needed with dx
+ *                and a pre norm; y where there is a post norm, or a gate whose gradient is asked for)
+ * Each output may be NULL: dh (type h_dtype; gradient of h), dy (type x_dtype), and fp32 sums over the tokens:
+ *   d_post_weight, d_post_bias, d_pre_weight, d_pre_bias [n], and d_gate [rows of gate x n], densely stored.
+ * dh may be dh_out itself (same leading dimension).  The normalised values are recomputed from h_new and y
+ * as they are stored; sums over the tokens are taken in fp32 in an order that depends on T, n and
+ * gate_tokens only, so the results are reproducible.
+ *   workspace  dev, 16-byte aligned, vnm_residual_norm_backward_workspace_bytes bytes; contents are scratch
+ * T == 0: the sums are set to zero (d_gate, of no rows unless gate_tokens is 0, likewise).
+ */
+typedef struct vnm_residual_norm_backward_args {
+  int64_t T, n;
+  int h_dtype, x_dtype, post, pre;
+  float residual_scale;
+  int64_t gate_tokens;
+  const void *dx, *dh_out, *h_new, *y, *gate, *post_weight, *post_bias, *pre_weight, *stats;
+  int64_t lddx, lddho, ldh, ldy, ldg;
+  void *dh, *dy, *d_post_weight, *d_post_bias, *d_pre_weight, *d_pre_bias, *d_gate;
+  int64_t lddh, lddy;
+} vnm_residual_norm_backward_args;
+int vnm_residual_norm_backward(const vnm_residual_norm_backward_args* a, void* workspace, int64_t workspace_bytes,
+                               void* stream);
+int vnm_residual_norm_backward_workspace_bytes(int64_t T, int64_t n, int64_t gate_tokens, int64_t* bytes);
+
 const char* vnm_status_string(int status);
 /* Text of the last HIP error seen by the calling thread ("" if none). */
 const char* vnm_last_hip_error(void);

@@ -6,6 +6,7 @@ import ctypes
 import functools
 import os
 from dataclasses import dataclass
+from typing import NamedTuple
 
 PATH_AUTO, PATH_GENERIC, PATH_SMFMAC = 0, 1, 2
 
@@ -23,6 +24,23 @@ class VnmSizes(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in (
         "out_pad", "in_pad", "row_blocks", "col_blocks", "kc", "values_elems", "meta_bytes",
         "colidx_bytes", "packed_bytes", "workspace_bytes")]
+
+
+def _struct(name, *groups):
+    """A ctypes structure from (type, "field field ...") pairs."""
+    return type(name, (ctypes.Structure,), {"_fields_": [(f, t) for t, names in groups for f in names.split()]})
+
+
+_I64, _INT, _F32, _PTR = ctypes.c_int64, ctypes.c_int, ctypes.c_float, ctypes.c_void_p
+_ResidualNormArgs = _struct(
+    "_ResidualNormArgs", (_I64, "T n"), (_INT, "h_dtype x_dtype post pre"), (_F32, "post_eps pre_eps residual_scale"),
+    (_I64, "gate_tokens"), (_PTR, "h y gate post_weight post_bias pre_weight pre_bias"), (_I64, "ldh ldy ldg"),
+    (_PTR, "h_out x q q_scale stats"), (_I64, "ldho ldx ldq"))
+_ResidualNormBackwardArgs = _struct(
+    "_ResidualNormBackwardArgs", (_I64, "T n"), (_INT, "h_dtype x_dtype post pre"), (_F32, "residual_scale"),
+    (_I64, "gate_tokens"), (_PTR, "dx dh_out h_new y gate post_weight post_bias pre_weight stats"),
+    (_I64, "lddx lddho ldh ldy ldg"), (_PTR, "dh dy d_post_weight d_post_bias d_pre_weight d_pre_bias d_gate"),
+    (_I64, "lddh lddy"))
 
 
 def lib_path() -> str:
@@ -108,6 +126,19 @@ def load_library():
     lib.vnm_spmm_scratch_bytes.restype = ci
     for f in (lib.vnm_query_sizes, lib.vnm_prune_compress, lib.vnm_pack, lib.vnm_spmm, lib.vnm_decompress,
               lib.vnm_format_version):
+        f.restype = ci
+    lib.vnm_quantize_x.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp, vp]
+    lib.vnm_i8_packed_bytes.argtypes = [i64, i64, ci, ci, ci, ctypes.POINTER(i64)]
+    lib.vnm_quantize_compressed.argtypes = [vp, vp, vp, i64, i64, ci, ci, ci, vp, vp, vp, vp]
+    lib.vnm_pack_i8.argtypes = [vp, vp, vp, i64, i64, ci, ci, ci, vp, vp]
+    lib.vnm_spmm_i8.argtypes = [vp, i64, i64, vp, vp, vp, vp, vp, vp, i64, i64, ci, ci, ci, vp, vp, i64, ci, ci, vp, i64, vp]
+    lib.vnm_spmm_i8_workspace_bytes.argtypes = [i64, i64, i64, ci, ci, ci, ctypes.POINTER(i64)]
+    lib.vnm_residual_norm.argtypes = [ctypes.POINTER(_ResidualNormArgs), vp]
+    lib.vnm_residual_norm_backward.argtypes = [ctypes.POINTER(_ResidualNormBackwardArgs), vp, i64, vp]
+    lib.vnm_residual_norm_backward_workspace_bytes.argtypes = [i64, i64, i64, ctypes.POINTER(i64)]
+    for f in (lib.vnm_quantize_x, lib.vnm_i8_packed_bytes, lib.vnm_quantize_compressed, lib.vnm_pack_i8, lib.vnm_spmm_i8,
+              lib.vnm_spmm_i8_workspace_bytes, lib.vnm_residual_norm, lib.vnm_residual_norm_backward,
+              lib.vnm_residual_norm_backward_workspace_bytes):
         f.restype = ci
     lib.vnm_status_string.argtypes = [ci]
     lib.vnm_status_string.restype = ctypes.c_char_p
@@ -575,3 +606,274 @@ def vnm_select_vm(candidates, threshold: float) -> int:
     sel = ctypes.c_int(-1)
     _check(load_library().vnm_select_vm(V, M, sp, n, float(threshold), ctypes.byref(sel)), "vnm_select_vm")
     return sel.value
+
+
+# --- layers in 8-bit integers and the norms between them ---------------------------------------------------------------
+
+_DTYPES = None
+
+
+def _dtype_code(dtype) -> int:
+    """The vnm_dtype of a torch type; raises for one that the library does not take."""
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float16: 0, torch.float32: 1, torch.bfloat16: 2}
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise VnmError(3, f"unsupported V:N:M, dtype or path: {dtype}")
+    return code
+
+
+def _launch(what: str, fn, device, *args):
+    """fn(*args, stream) on the device's current stream, with that device current."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        status = fn(*args, _raw_stream(device))
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, _raw_stream(device))
+    if status:
+        _check(status, what)
+
+
+def _rows(name, t, T, n, device, dtype=None):
+    """Checks a [T x n] tensor with rows of consecutive elements; returns its leading dimension."""
+    assert t.device == device and t.dim() == 2 and t.shape[0] == T and t.shape[1] == n, name
+    assert dtype is None or t.dtype == dtype, name
+    assert T == 0 or n == 1 or t.stride(1) == 1, name
+    ld = t.stride(0) if T > 1 else n
+    assert T <= 1 or ld >= n, name
+    return ld
+
+
+def _vector(name, t, n, device, dtype):
+    assert t is None or (t.device == device and t.dtype == dtype and t.shape == (n,) and t.is_contiguous()), name
+    return 0 if t is None else t.data_ptr()
+
+
+def _empty_i8_rows(T: int, n: int, device):
+    """int8 [T x n] with rows 16 bytes aligned, as the matrix-core kernels read them."""
+    import torch
+    ld = (n + 15) // 16 * 16
+    q = torch.empty((T, ld), dtype=torch.int8, device=device)
+    return q if ld == n else q[:, :n]
+
+
+def vnm_quantize_x(X, Q=None, scale=None):
+    """int8 activations with one scale per token: (Q int8 [T x n], scale fp32 [T]) of X [T x n] (fp16, bf16 or fp32),
+    Q = rint(X * (127 / max|X_t|)), scale = max|X_t| / 127.  A fresh Q has rows 16 bytes aligned."""
+    import torch
+    assert X.is_cuda and X.dim() == 2
+    T, n = X.shape
+    dev = X.device
+    ldx = _rows("X", X, T, n, dev)
+    if Q is None:
+        Q = _empty_i8_rows(T, n, dev)
+    if scale is None:
+        scale = torch.empty(T, dtype=torch.float32, device=dev)
+    ldq = _rows("Q", Q, T, n, dev, torch.int8)
+    _launch("vnm_quantize_x", load_library().vnm_quantize_x, dev, X.data_ptr(), T, n, ldx, _dtype_code(X.dtype), Q.data_ptr(),
+            ldq, _vector("scale", scale, T, dev, torch.float32))
+    return Q, scale
+
+
+@dataclass
+class CompressedI8:
+    """A compressed layer in 8 bits (device tensors): int8 values in the order of Compressed.values, its positions and column
+    indices, the opaque matrix-core copy, and one fp32 scale per output channel."""
+    values: object
+    meta: object
+    colidx: object
+    packed: object
+    scale: object
+    out: int
+    inn: int
+    V: int
+    M: int
+
+
+def _i8_packed(c: CompressedI8, N: int):
+    import torch
+    b = ctypes.c_int64(0)
+    _check(load_library().vnm_i8_packed_bytes(c.out, c.inn, c.V, N, c.M, ctypes.byref(b)), "vnm_i8_packed_bytes")
+    return torch.empty(b.value, dtype=torch.uint8, device=c.values.device) if b.value > 0 else None
+
+
+def _check_triple(values, dtype, c, N):
+    import torch
+    s = vnm_query_sizes(c.out, c.inn, c.V, c.M, N)
+    for name, t, dt, n in (("values", values, dtype, s.values_elems), ("meta", c.meta, torch.uint8, s.meta_bytes),
+                           ("colidx", c.colidx, torch.uint8, s.colidx_bytes)):
+        assert t.is_cuda and t.device == values.device and t.dtype == dt and t.is_contiguous() and t.numel() == n, name
+    return s
+
+
+def vnm_quantize_compressed(c: Compressed, N: int = 2) -> CompressedI8:
+    """The layer's kept values in 8 bits, one scale per output channel; meta and colidx are shared with `c`."""
+    import torch
+    s = _check_triple(c.values, torch.float16, c, N)
+    dev = c.values.device
+    q = CompressedI8(torch.empty(s.values_elems, dtype=torch.int8, device=dev), c.meta, c.colidx, None,
+                     torch.empty(c.out, dtype=torch.float32, device=dev), c.out, c.inn, c.V, c.M)
+    q.packed = _i8_packed(q, N)
+    _launch("vnm_quantize_compressed", load_library().vnm_quantize_compressed, dev, _ptr(c.values), _ptr(c.meta),
+            _ptr(c.colidx), c.out, c.inn, c.V, N, c.M, _ptr(q.values), _ptr(q.scale), _ptr(q.packed))
+    return q
+
+
+def vnm_pack_i8(c: CompressedI8, N: int = 2) -> CompressedI8:
+    """Fills c.packed from the triple (allocated where it is None and this V, M has one)."""
+    import torch
+    _check_triple(c.values, torch.int8, c, N)
+    if c.packed is None:
+        c.packed = _i8_packed(c, N)
+    if c.packed is not None:
+        _launch("vnm_pack_i8", load_library().vnm_pack_i8, c.values.device, _ptr(c.values), _ptr(c.meta), _ptr(c.colidx), c.out,
+                c.inn, c.V, N, c.M, _ptr(c.packed))
+    return c
+
+
+@functools.lru_cache(maxsize=1024, typed=True)      # (typed: 16.0 is refused, also after 16)
+def _spmm_i8_workspace_bytes(T: int, out: int, inn: int, V: int, N: int, M: int) -> int:
+    b = ctypes.c_int64(0)
+    _check(load_library().vnm_spmm_i8_workspace_bytes(T, out, inn, V, N, M, ctypes.byref(b)), "vnm_spmm_i8_workspace_bytes")
+    return b.value
+
+
+def vnm_spmm_i8_workspace_bytes(T: int, c: CompressedI8, N: int = 2) -> int:
+    return _spmm_i8_workspace_bytes(T, c.out, c.inn, c.V, N, c.M)
+
+
+def vnm_spmm_i8(Q, scale, c: CompressedI8, bias=None, N: int = 2, out_dtype=None, path: int = PATH_AUTO, Y=None, workspace=None):
+    """Y [T x out] = (Q . Wq^T) * c.scale[o] * scale[t] + bias[o], sums exact in int32, Y in fp16, bf16 or fp32 (default fp16).
+    Q, scale as vnm_quantize_x leaves them; `bias` fp16 [out].  `workspace`: optional uint8 CUDA tensor of at least
+    vnm_spmm_i8_workspace_bytes(T, c) bytes; by default the call takes one from torch's allocator."""
+    import torch
+    assert Q.is_cuda and Q.dim() == 2
+    T, dev = Q.shape[0], Q.device
+    ldq = _rows("Q", Q, T, c.inn, dev, torch.int8)
+    if T == 1:
+        ldq = (c.inn + 15) // 16 * 16            # (one row: whatever the view's stride)
+    assert c.values.device == dev and c.scale.device == dev
+    if Y is None:
+        Y = torch.empty((T, c.out), dtype=out_dtype or torch.float16, device=dev)
+    ldy = _rows("Y", Y, T, c.out, dev)
+    need = 0 if path == PATH_GENERIC or c.packed is None else _spmm_i8_workspace_bytes(T, c.out, c.inn, c.V, N, c.M)
+    if need and workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    _launch("vnm_spmm_i8", load_library().vnm_spmm_i8, dev, Q.data_ptr(), T, ldq, _vector("scale", scale, T, dev, torch.float32),
+            _ptr(c.values), _ptr(c.meta), _ptr(c.colidx), _ptr(c.packed), _vector("c.scale", c.scale, c.out, dev, torch.float32),
+            c.out, c.inn, c.V, N, c.M, _vector("bias", bias, c.out, dev, torch.float16), Y.data_ptr(), ldy, _dtype_code(Y.dtype),
+            path, _ptr(workspace), 0 if workspace is None else workspace.numel())
+    return Y
+
+
+_NORMS = {"none": 0, "rms": 1, "layer": 2}
+
+
+class ResidualNorm(NamedTuple):
+    """What vnm_residual_norm returns: the new residual stream, the normalised rows (or their int8 values with `scale`), and
+    the statistics that vnm_residual_norm_backward takes."""
+    h: object
+    x: object
+    scale: object
+    stats: object
+
+
+class ResidualNormGrads(NamedTuple):
+    h: object
+    y: object
+    gate: object
+    post_weight: object
+    post_bias: object
+    pre_weight: object
+    pre_bias: object
+
+
+def _norm_operands(h, y, gate, gate_tokens, post, pre, x_dtype, vectors):
+    """Shared checks of the two norm calls: (T, n, device, x type, leading dimensions of h, y and gate)."""
+    assert h.is_cuda and h.dim() == 2
+    T, n = h.shape
+    dev = h.device
+    if x_dtype is None:
+        x_dtype = next((t.dtype for t in (y, *vectors) if t is not None), h.dtype)
+    ldh = _rows("h", h, T, n, dev)
+    ldy = 0 if y is None else _rows("y", y, T, n, dev, x_dtype)
+    ldg = 0
+    if gate is not None:
+        assert gate_tokens >= 0, "gate_tokens"
+        if gate_tokens == 0:
+            _vector("gate", gate, n, dev, x_dtype)
+        else:
+            ldg = _rows("gate", gate, -(-T // gate_tokens), n, dev, x_dtype)
+    return T, n, dev, x_dtype, ldh, ldy, ldg
+
+
+def vnm_residual_norm(h, y=None, gate=None, gate_tokens: int = 0, residual_scale: float = 1.0, post: str = "none",
+                      post_weight=None, post_bias=None, post_eps: float = 1e-5, pre: str = "none", pre_weight=None,
+                      pre_bias=None, pre_eps: float = 1e-5, x_dtype=None, int8: bool = False, want_x: bool = True,
+                      want_stats: bool = False, h_out=None) -> ResidualNorm:
+    """Between two blocks: h' = residual_scale * h + gate * norm_post(y), x = norm_pre(h').
+
+    h [T x n] is the residual stream (type of y, or fp32), y [T x n] the block's output (None: only h).  `gate`: [n], or with
+    gate_tokens > 0 one row per that many tokens.  post, pre: "none", "rms" or "layer".  Weights, biases and gate have y's type,
+    which is x's too (`x_dtype` where there is none of them).  int8: x leaves as int8 rows with a scale per token, ready for
+    vnm_spmm_i8.  h_out: a tensor for h' (h itself: in place); a fresh one by default."""
+    import torch
+    T, n, dev, xt, ldh, ldy, ldg = _norm_operands(h, y, gate, gate_tokens, post, pre, x_dtype,
+                                                  (post_weight, post_bias, pre_weight, pre_bias))
+    if h_out is None:
+        h_out = torch.empty((T, n), dtype=h.dtype, device=dev)
+    ldho = _rows("h_out", h_out, T, n, dev, h.dtype)
+    x = q = scale = stats = None
+    if want_x and int8:
+        q, scale = _empty_i8_rows(T, n, dev), torch.empty(T, dtype=torch.float32, device=dev)
+    elif want_x:
+        x = torch.empty((T, n), dtype=xt, device=dev)
+    if want_stats:
+        stats = torch.empty((T, 4), dtype=torch.float32, device=dev)
+    a = _ResidualNormArgs(
+        T, n, _dtype_code(h.dtype), _dtype_code(xt), _NORMS[post], _NORMS[pre], post_eps, pre_eps, residual_scale, gate_tokens,
+        h.data_ptr(), _ptr(y), _ptr(gate), _vector("post_weight", post_weight, n, dev, xt), _vector("post_bias", post_bias, n, dev, xt),
+        _vector("pre_weight", pre_weight, n, dev, xt), _vector("pre_bias", pre_bias, n, dev, xt), ldh, ldy, ldg,
+        h_out.data_ptr(), _ptr(x), _ptr(q), _ptr(scale), _ptr(stats), ldho, n, (n + 15) // 16 * 16)
+    _launch("vnm_residual_norm", load_library().vnm_residual_norm, dev, ctypes.byref(a))
+    return ResidualNorm(h_out, q if int8 else x, scale, stats)
+
+
+def vnm_residual_norm_backward(h, stats, dx=None, dh=None, y=None, gate=None, gate_tokens: int = 0, residual_scale: float = 1.0,
+                               post: str = "none", post_weight=None, post_bias=None, pre: str = "none", pre_weight=None,
+                               pre_bias=None, want_dh: bool = True, want_dy: bool = True, want_params: bool = True,
+                               workspace=None) -> ResidualNormGrads:
+    """Gradients of vnm_residual_norm from dx and dh, those of its results x and h (either may be None).  `h` and `stats` are
+    what the forward call returned (its h, with want_stats), everything else what it was given.  Sums over the tokens (weights,
+    biases, gate) come in fp32; the gradient of an argument that is None is None."""
+    import torch
+    T, n, dev, xt, ldh, ldy, ldg = _norm_operands(h, y, gate, gate_tokens, post, pre, None if dx is None else dx.dtype,
+                                                  (post_weight, post_bias, pre_weight, pre_bias, gate))
+    lddx = 0 if dx is None else _rows("dx", dx, T, n, dev, xt)
+    lddho = 0 if dh is None else _rows("dh", dh, T, n, dev, h.dtype)
+    assert stats is None or (stats.shape == (T, 4) and stats.dtype == torch.float32 and stats.is_contiguous() and stats.device == dev)
+    empty = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=dev)
+    gh = empty((T, n), h.dtype) if want_dh else None
+    gy = empty((T, n), xt) if want_dy and y is not None else None
+    vec = lambda t: empty((n,), torch.float32) if want_params and t is not None else None
+    g_pw, g_pb = vec(pre_weight) if dx is not None else None, vec(pre_bias) if dx is not None else None
+    g_ow, g_ob = vec(post_weight), vec(post_bias)
+    g_gate = empty(gate.shape, torch.float32) if want_params and gate is not None else None
+    lib = load_library()
+    if workspace is None and any(t is not None for t in (g_pw, g_pb, g_ow, g_ob, g_gate)):
+        b = ctypes.c_int64(0)
+        _check(lib.vnm_residual_norm_backward_workspace_bytes(T, n, gate_tokens if gate is not None else 0, ctypes.byref(b)),
+               "vnm_residual_norm_backward_workspace_bytes")
+        workspace = torch.empty(b.value, dtype=torch.uint8, device=dev)
+    a = _ResidualNormBackwardArgs(
+        T, n, _dtype_code(h.dtype), _dtype_code(xt), _NORMS[post], _NORMS[pre], residual_scale, gate_tokens if gate is not None else 0,
+        _ptr(dx), _ptr(dh), h.data_ptr(), _ptr(y), _ptr(gate), _vector("post_weight", post_weight, n, dev, xt),
+        _vector("post_bias", post_bias, n, dev, xt), _vector("pre_weight", pre_weight, n, dev, xt), _ptr(stats), lddx, lddho, ldh, ldy,
+        ldg, _ptr(gh), _ptr(gy), _ptr(g_ow), _ptr(g_ob), _ptr(g_pw), _ptr(g_pb), _ptr(g_gate), n, n)
+    _vector("pre_bias", pre_bias, n, dev, xt)
+    _launch("vnm_residual_norm_backward", lib.vnm_residual_norm_backward, dev, ctypes.byref(a), _ptr(workspace),
+            0 if workspace is None else workspace.numel())
+    return ResidualNormGrads(gh, gy, g_gate, g_ow, g_ob, g_pw, g_pb)

@@ -1,0 +1,88 @@
+// Row operations of the norm kernels (vnm_norm.hip, vnm_norm_backward.hip).
+#pragma once
+#include "vnm_i8.h"
+
+namespace vnm {
+
+// 8 consecutive elements as they are stored: one 16-byte load for 16-bit types, two for fp32
+template <typename T> struct alignas(16) Octet { T v[8]; };
+
+// The share of a row that a thread of TPR holds: octets tid, tid + TPR, ...  VEC: rows are 16-byte aligned and n % 8 == 0, so
+// that an octet is inside the row or outside as a whole; otherwise its elements are fetched and stored one by one.
+template <typename T, int TPR, int NCH>
+__device__ __forceinline__ void load_row(const T* p, int n, int tid, bool vec, Octet<T> (&r)[NCH]) {
+  if (vec) {
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      const int at = (c * TPR + tid) * 8;
+      if (at < n) r[c] = *(const Octet<T>*)(p + at);
+      else r[c] = Octet<T>{};
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int at = (c * TPR + tid) * 8 + e;
+        r[c].v[e] = at < n ? p[at] : (T)0.f;
+      }
+  }
+}
+template <typename T, int TPR, int NCH>
+__device__ __forceinline__ void store_row(T* p, int n, int tid, bool vec, const float (&x)[NCH][8]) {
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) {
+    const int at = (c * TPR + tid) * 8;
+    Octet<T> o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o.v[e] = (T)x[c][e];
+    if (vec) { if (at < n) *(Octet<T>*)(p + at) = o; }
+    else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (at + e < n) p[at + e] = o.v[e];
+    }
+  }
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
+  return v;
+}
+__device__ __forceinline__ unsigned wave_max(unsigned v) {
+#pragma unroll
+  for (int m = 32; m; m >>= 1) { const unsigned w = __shfl_xor(v, m); v = w > v ? w : v; }
+  return v;
+}
+// Over the TPR threads that share a row.  `lds`: two halves of TPR / 64 pairs, used in turn (`turn`), so that one barrier per
+// reduction is enough: a wave reaches the use after next of a half only past the barrier of the next.
+template <int TPR>
+__device__ __forceinline__ float2 row_sum2(float a, float b, float2* lds, int& turn) {
+  a = wave_sum(a); b = wave_sum(b);
+  if (TPR == 64) return make_float2(a, b);
+  constexpr int W = TPR / 64;
+  float2* half = lds + (turn & 1) * W;
+  ++turn;
+  if ((threadIdx.x & 63) == 0) half[threadIdx.x >> 6] = make_float2(a, b);
+  __syncthreads();
+  float2 s = half[0];
+#pragma unroll
+  for (int w = 1; w < W; ++w) { s.x += half[w].x; s.y += half[w].y; }
+  return s;
+}
+template <int TPR>
+__device__ __forceinline__ unsigned row_max(unsigned v, float2* lds, int& turn) {
+  v = wave_max(v);
+  if (TPR == 64) return v;
+  constexpr int W = TPR / 64;
+  unsigned* half = (unsigned*)(lds + (turn & 1) * W);
+  ++turn;
+  if ((threadIdx.x & 63) == 0) half[threadIdx.x >> 6] = v;
+  __syncthreads();
+  unsigned m = half[0];
+#pragma unroll
+  for (int w = 1; w < W; ++w) m = half[w] > m ? half[w] : m;
+  return m;
+}
+
+}  // namespace vnm

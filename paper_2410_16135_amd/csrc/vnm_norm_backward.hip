@@ -1,0 +1,311 @@
+// Gradients of vnm_residual_norm.
+//
+// With xhat = (h' - mean) r, g = dx * weight, a row's gradient through a norm is r (g - mean(g) - xhat mean(g xhat)) (without
+// the mean of g for VNM_NORM_RMS), so a row needs two sums per norm; the gradients of weights, biases and gates are sums over
+// the tokens.  One pass over the tokens does both: a worker (the threads that share a row) owns a run of consecutive tokens of
+// one gate row, keeps its share of the column sums in registers, and leaves them at the end as one row of partial sums in the
+// workspace; a second kernel adds the workers' rows in a fixed order.
+#include "vnm_norm.h"
+
+namespace vnm {
+
+enum { kPreWeight, kPreBias, kPostWeight, kPostBias, kGate, kSums };
+
+// How the tokens are cut: `groups` gate rows (1 without) of `tokens` tokens each, `pieces` runs of `per` tokens per group.
+struct Cut { int64_t groups, tokens, pieces, per; };
+
+static Cut make_cut(int64_t T, int64_t n, int64_t gate_tokens) {
+  Cut c;
+  c.tokens = gate_tokens > 0 && gate_tokens < T ? gate_tokens : T > 0 ? T : 1;
+  c.groups = T > 0 ? (T + c.tokens - 1) / c.tokens : 0;
+  const int64_t workers = n <= 1024 ? 2048 : 512;
+  c.per = (T + workers - 1) / workers;
+  if (c.per < 1) c.per = 1;
+  if (c.per > c.tokens) c.per = c.tokens;
+  c.pieces = (c.tokens + c.per - 1) / c.per;
+  return c;
+}
+
+struct BackArgs {
+  vnm_residual_norm_backward_args a;
+  Cut cut;
+  float* part;            // [kSums][workers][n]; a sum that is not asked for has no room of its own
+  int64_t part_at[kSums];
+  int vec;
+};
+
+template <typename HT, typename XT, int TPR, int NCH>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
+residual_norm_backward_kernel(const BackArgs b) {
+  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
+  __shared__ float2 lds[TPR == 64 ? 1 : 2 * (TPR / 64)];
+  int turn = 0;
+  const vnm_residual_norm_backward_args& a = b.a;
+  const int tid = TPR == 64 ? (threadIdx.x & 63) : threadIdx.x;
+  const int64_t worker = (int64_t)blockIdx.x * RPB + (TPR == 64 ? threadIdx.x >> 6 : 0);
+  if (worker >= b.cut.groups * b.cut.pieces) return;     // a whole worker: those of one wave share no barrier
+  const int64_t group = worker / b.cut.pieces, first = group * b.cut.tokens + (worker - group * b.cut.pieces) * b.cut.per;
+  int64_t end = first + b.cut.per;
+  const int64_t group_end = (group + 1) * b.cut.tokens < a.T ? (group + 1) * b.cut.tokens : a.T;
+  end = end < group_end ? end : group_end;
+  const int n = (int)a.n;
+  const float inv_n = 1.f / (float)n;
+  const bool vec = b.vec;
+  Octet<XT> pw[NCH], ow[NCH], ob[NCH], gt[NCH];
+  if (a.pre_weight) load_row<XT, TPR, NCH>((const XT*)a.pre_weight, n, tid, vec, pw);
+  if (a.post_weight) load_row<XT, TPR, NCH>((const XT*)a.post_weight, n, tid, vec, ow);
+  if (a.post_bias) load_row<XT, TPR, NCH>((const XT*)a.post_bias, n, tid, vec, ob);
+  if (a.gate) load_row<XT, TPR, NCH>((const XT*)a.gate + group * a.ldg, n, tid, vec, gt);
+  float sum[kSums][NCH][8];
+#pragma unroll
+  for (int k = 0; k < kSums; ++k)
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[k][c][e] = 0.f;
+  const bool through_pre = a.dx && a.pre != VNM_NORM_NONE;
+  for (int64_t t = first; t < end; ++t) {
+    Octet<XT> xr[NCH], yr[NCH];
+    Octet<HT> hr[NCH], gr[NCH];
+    if (a.dx) load_row<XT, TPR, NCH>((const XT*)a.dx + t * a.lddx, n, tid, vec, xr);
+    if (through_pre) load_row<HT, TPR, NCH>((const HT*)a.h_new + t * a.ldh, n, tid, vec, hr);
+    if (a.dh_out) load_row<HT, TPR, NCH>((const HT*)a.dh_out + t * a.lddho, n, tid, vec, gr);
+    if (a.y) load_row<XT, TPR, NCH>((const XT*)a.y + t * a.ldy, n, tid, vec, yr);
+    float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
+    if (a.stats) st = ((const float4*)a.stats)[t];
+    // d = gradient of h'
+    float d[NCH][8];
+    if (through_pre) {
+      float xhat[NCH][8], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float dx = (float)xr[c].v[e];
+          xhat[c][e] = ((float)hr[c].v[e] - st.z) * st.w;
+          sum[kPreWeight][c][e] += dx * xhat[c][e];
+          sum[kPreBias][c][e] += dx;
+          d[c][e] = a.pre_weight ? dx * (float)pw[c].v[e] : dx;
+          s1 += d[c][e] * xhat[c][e];                    // (dx is 0 outside the row)
+          s2 += d[c][e];
+        }
+      const float2 s = row_sum2<TPR>(s1, s2, lds, turn);
+      const float m1 = s.x * inv_n, m2 = a.pre == VNM_NORM_LAYER ? s.y * inv_n : 0.f;
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[c][e] = st.w * (d[c][e] - m2 - xhat[c][e] * m1);
+    } else {
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[c][e] = a.dx ? (float)xr[c].v[e] : 0.f;
+    }
+    if (a.dh_out) {
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[c][e] += (float)gr[c].v[e];
+    }
+    if (a.dh) {
+      float o[NCH][8];
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[c][e] = a.residual_scale * d[c][e];
+      store_row<HT, TPR, NCH>((HT*)a.dh + t * a.lddh, n, tid, vec, o);
+    }
+    if (!a.dy && !a.d_gate && !a.d_post_weight && !a.d_post_bias) continue;
+    // through the gate and the post norm
+    float yhat[NCH][8], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        yhat[c][e] = a.y ? ((float)yr[c].v[e] - st.x) * st.y : 0.f;
+        const bool inside = (c * TPR + tid) * 8 + e < n;
+        if (!inside) d[c][e] = yhat[c][e] = 0.f;         // (the means were taken away outside the row too)
+        if (a.d_gate) {
+          float p = yhat[c][e];
+          if (a.post_weight) p *= (float)ow[c].v[e];
+          if (a.post_bias) p += (float)ob[c].v[e];
+          sum[kGate][c][e] += d[c][e] * p;
+        }
+        if (a.gate) d[c][e] *= (float)gt[c].v[e];
+        if (a.post != VNM_NORM_NONE) {
+          sum[kPostWeight][c][e] += d[c][e] * yhat[c][e];
+          sum[kPostBias][c][e] += d[c][e];
+          if (a.post_weight) d[c][e] *= (float)ow[c].v[e];
+          s1 += d[c][e] * yhat[c][e];
+          s2 += d[c][e];
+        }
+      }
+    if (!a.dy) continue;
+    if (a.post != VNM_NORM_NONE) {
+      const float2 s = row_sum2<TPR>(s1, s2, lds, turn);
+      const float m1 = s.x * inv_n, m2 = a.post == VNM_NORM_LAYER ? s.y * inv_n : 0.f;
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[c][e] = st.y * (d[c][e] - m2 - yhat[c][e] * m1);
+    }
+    store_row<XT, TPR, NCH>((XT*)a.dy + t * a.lddy, n, tid, vec, d);
+  }
+  // the worker's row of every sum that is asked for
+#pragma unroll
+  for (int k = 0; k < kSums; ++k) {
+    if (b.part_at[k] < 0) continue;
+    float* p = b.part + b.part_at[k] + worker * n;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      const int at = (c * TPR + tid) * 8;
+      if (n % 8 == 0) {
+        if (at < n) {
+          *(float4*)(p + at) = make_float4(sum[k][c][0], sum[k][c][1], sum[k][c][2], sum[k][c][3]);
+          *(float4*)(p + at + 4) = make_float4(sum[k][c][4], sum[k][c][5], sum[k][c][6], sum[k][c][7]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (at + e < n) p[at + e] = sum[k][c][e];
+      }
+    }
+  }
+}
+
+// out[row][i] = sum over the `count` rows of part from row * count on: 32 columns per workgroup, 8 threads per column
+struct ReduceArgs { const float* part[kSums]; float* out[kSums]; int64_t rows[kSums], count[kSums]; int64_t n; };
+__global__ void __launch_bounds__(256) column_reduce_kernel(const ReduceArgs r) {
+  __shared__ float lds[8][33];
+  const int col = threadIdx.x & 31, slice = threadIdx.x >> 5;
+  const int64_t i = (int64_t)blockIdx.x * 32 + col;
+  const int k = blockIdx.z;
+  for (int64_t row = blockIdx.y; row < r.rows[k]; row += gridDim.y) {
+    const int64_t count = r.count[k];
+    const float* p = r.part[k] + row * count * r.n;
+    float s = 0.f;
+    if (i < r.n)
+      for (int64_t w = slice; w < count; w += 8) s += p[w * r.n + i];
+    lds[slice][col] = s;
+    __syncthreads();
+    if (slice == 0 && i < r.n) {
+#pragma unroll
+      for (int q = 1; q < 8; ++q) s += lds[q][col];
+      r.out[k][row * r.n + i] = s;
+    }
+    __syncthreads();
+  }
+}
+
+template <typename HT, typename XT, int TPR, int NCH>
+static int launch_back_cfg(const BackArgs& b, hipStream_t st) {
+  constexpr int RPB = TPR < 256 ? 256 / TPR : 1, THREADS = TPR < 256 ? 256 : TPR;
+  const int64_t blocks = (b.cut.groups * b.cut.pieces + RPB - 1) / RPB;
+  if (blocks > 0x7FFFFFFF) return VNM_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL((residual_norm_backward_kernel<HT, XT, TPR, NCH>), dim3((unsigned)blocks), dim3(THREADS), 0, st, b);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) { set_hip_error(e, "residual_norm_backward_kernel"); return VNM_ERR_HIP; }
+  return VNM_OK;
+}
+template <typename HT, typename XT>
+static int launch_back(const BackArgs& b, hipStream_t st) {
+  if (b.a.n <= 512) return launch_back_cfg<HT, XT, 64, 1>(b, st);
+  if (b.a.n <= 1024) return launch_back_cfg<HT, XT, 64, 2>(b, st);
+  if (b.a.n <= 2048) return launch_back_cfg<HT, XT, 256, 1>(b, st);
+  if (b.a.n <= 4096) return launch_back_cfg<HT, XT, 512, 1>(b, st);
+  if (b.a.n <= 8192) return launch_back_cfg<HT, XT, 512, 2>(b, st);
+  return launch_back_cfg<HT, XT, 1024, 2>(b, st);
+}
+
+static int64_t gate_rows(int64_t T, int64_t gate_tokens) { return gate_tokens > 0 ? (T + gate_tokens - 1) / gate_tokens : 1; }
+
+}  // namespace vnm
+
+using namespace vnm;
+
+static bool dtype_ok(int t) { return t == VNM_F16 || t == VNM_F32 || t == VNM_BF16; }
+static uintptr_t dtype_bytes(int t) { return t == VNM_F32 ? 4 : 2; }
+
+extern "C" int vnm_residual_norm_backward_workspace_bytes(int64_t T, int64_t n, int64_t gate_tokens, int64_t* bytes) {
+  if (!bytes) return VNM_ERR_NULL;
+  if (T < 0 || n <= 0 || gate_tokens < 0) return VNM_ERR_SHAPE;
+  if (n > VNM_NORM_MAX_CHANNELS) return VNM_ERR_UNSUPPORTED;
+  const Cut c = make_cut(T, n, gate_tokens);
+  const int64_t each = (c.groups * c.pieces * n * 4 + 255) / 256 * 256;
+  *bytes = kSums * each + 256;
+  return VNM_OK;
+}
+
+extern "C" int vnm_residual_norm_backward(const vnm_residual_norm_backward_args* args, void* workspace, int64_t workspace_bytes,
+                                          void* stream) {
+  if (!args) return VNM_ERR_NULL;
+  const vnm_residual_norm_backward_args& a = *args;
+  if (a.T < 0 || a.n <= 0 || a.gate_tokens < 0) return VNM_ERR_SHAPE;
+  if (a.n > VNM_NORM_MAX_CHANNELS) return VNM_ERR_UNSUPPORTED;
+  if (!dtype_ok(a.x_dtype) || !(a.h_dtype == a.x_dtype || a.h_dtype == VNM_F32)) return VNM_ERR_UNSUPPORTED;
+  if (a.post < VNM_NORM_NONE || a.post > VNM_NORM_LAYER || a.pre < VNM_NORM_NONE || a.pre > VNM_NORM_LAYER) return VNM_ERR_UNSUPPORTED;
+  const bool has_post = a.post != VNM_NORM_NONE, has_pre = a.pre != VNM_NORM_NONE;
+  if (!has_post && (a.post_weight || a.post_bias || a.d_post_weight || a.d_post_bias)) return VNM_ERR_UNSUPPORTED;
+  if (!has_pre && (a.pre_weight || a.d_pre_weight || a.d_pre_bias)) return VNM_ERR_UNSUPPORTED;
+  if (workspace_bytes < 0) return VNM_ERR_WORKSPACE;
+  const bool past_gate = a.dy || a.d_post_weight || a.d_post_bias || a.d_gate;
+  const bool any_sum = a.d_pre_weight || a.d_pre_bias || a.d_post_weight || a.d_post_bias || a.d_gate;
+  if (!a.dh && !a.dy && !any_sum) return VNM_ERR_NULL;
+  if (a.T != 0) {
+    if (!a.dx && !a.dh_out) return VNM_ERR_NULL;
+    if ((a.dx && has_pre && (!a.h_new || !a.stats)) || (past_gate && has_post && (!a.y || !a.stats)) || (a.d_gate && !a.y))
+      return VNM_ERR_NULL;
+    if ((a.dx && a.lddx < a.n) || (a.dh_out && a.lddho < a.n) || (a.h_new && a.ldh < a.n) || (a.y && a.ldy < a.n) ||
+        (a.gate && a.gate_tokens && a.ldg < a.n) || (a.dh && a.lddh < a.n) || (a.dy && a.lddy < a.n) ||
+        (a.dh && a.dh == a.dh_out && a.lddh != a.lddho))
+      return VNM_ERR_SHAPE;
+  }
+  const uintptr_t hp = (uintptr_t)a.dh_out | (uintptr_t)a.h_new | (uintptr_t)a.dh;
+  const uintptr_t xp = (uintptr_t)a.dx | (uintptr_t)a.y | (uintptr_t)a.gate | (uintptr_t)a.post_weight | (uintptr_t)a.post_bias |
+                       (uintptr_t)a.pre_weight | (uintptr_t)a.dy;
+  const uintptr_t sp = (uintptr_t)a.d_post_weight | (uintptr_t)a.d_post_bias | (uintptr_t)a.d_pre_weight | (uintptr_t)a.d_pre_bias |
+                       (uintptr_t)a.d_gate;
+  if ((hp & (dtype_bytes(a.h_dtype) - 1)) || (xp & (dtype_bytes(a.x_dtype) - 1)) || (sp & 3) || ((uintptr_t)a.stats & 15) ||
+      ((uintptr_t)workspace & 15))
+    return VNM_ERR_ALIGN;
+  if (a.T != 0 && any_sum && !workspace) return VNM_ERR_WORKSPACE;
+  BackArgs b;
+  b.a = a;
+  b.cut = make_cut(a.T, a.n, a.gate_tokens);
+  const int64_t workers = b.cut.groups * b.cut.pieces, each = (workers * a.n * 4 + 255) / 256 * 256;
+  void* const outs[kSums] = {a.d_pre_weight, a.d_pre_bias, a.d_post_weight, a.d_post_bias, a.d_gate};
+  ReduceArgs r{};
+  r.n = a.n;
+  int asked = 0;
+  b.part = (float*)workspace;
+  for (int k = 0; k < kSums; ++k) {
+    b.part_at[k] = -1;
+    if (!outs[k]) continue;
+    b.part_at[k] = asked * (each / 4);
+    r.part[asked] = b.part + b.part_at[k];
+    r.out[asked] = (float*)outs[k];
+    r.rows[asked] = k == kGate ? gate_rows(a.T, a.gate_tokens) : 1;
+    r.count[asked] = k == kGate ? b.cut.pieces : workers;
+    ++asked;
+  }
+  if (a.T != 0 && asked && workspace_bytes < asked * each) return VNM_ERR_WORKSPACE;
+  if (a.T == 0) for (int k = 0; k < asked; ++k) r.count[k] = 0;       // the sums of no tokens
+  hipStream_t st = (hipStream_t)stream;
+  if (a.T != 0) {
+    const int64_t lds = (a.dx ? a.lddx : 0) | (a.dh_out ? a.lddho : 0) | (a.h_new ? a.ldh : 0) | (a.y ? a.ldy : 0) |
+                        (a.gate && a.gate_tokens ? a.ldg : 0) | (a.dh ? a.lddh : 0) | (a.dy ? a.lddy : 0);
+    b.vec = a.n % 8 == 0 && lds % 8 == 0 && ((hp | xp) & 15) == 0;
+    if (!a.gate_tokens) b.a.ldg = 0;
+    int rc;
+    if (a.x_dtype == VNM_F32) rc = launch_back<float, float>(b, st);
+    else if (a.h_dtype == VNM_F32) rc = a.x_dtype == VNM_F16 ? launch_back<float, _Float16>(b, st) : launch_back<float, __bf16>(b, st);
+    else rc = a.x_dtype == VNM_F16 ? launch_back<_Float16, _Float16>(b, st) : launch_back<__bf16, __bf16>(b, st);
+    if (rc) return rc;
+  }
+  if (!asked) return VNM_OK;
+  const int64_t rows = gate_rows(a.T, a.gate_tokens);
+  const unsigned gy = (unsigned)(a.d_gate && rows > 1 ? (rows < 65535 ? rows : 65535) : 1);
+  hipLaunchKernelGGL(column_reduce_kernel, dim3((unsigned)((a.n + 31) / 32), gy, (unsigned)asked), dim3(256), 0, st, r);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) { set_hip_error(e, "column_reduce_kernel"); return VNM_ERR_HIP; }
+  return VNM_OK;
+}
