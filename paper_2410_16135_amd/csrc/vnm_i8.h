@@ -79,5 +79,6 @@ int launch_quantize_rows(const void* X, int64_t T, int64_t n, int64_t ldx, int x
 int launch_pack_i8(const void* qvalues, const void* meta, const void* colidx, const Dims& d, void* packed, hipStream_t st);
 int launch_spmm_i8_triple(const void* Q, int64_t T, int64_t ldq, const void* qvalues, const void* meta, const void* colidx,
                           const Dims& d, const I8Epilogue& e, hipStream_t st);
+int launch_spmm_i8_few(const void* Q, int64_t T, int64_t ldq, const void* packed, const Dims& d, const I8Epilogue& e, hipStream_t st);
 
 }  // namespace vnm

@@ -185,9 +185,11 @@ extern "C" int vnm_spmm_i8(const void* Q, int64_t T, int64_t ldq, const void* sc
     return VNM_ERR_ALIGN;
   const Dims d = make_dims(out, in, V, M);
   if (!i8_sums_fit(d)) return VNM_ERR_UNSUPPORTED;
-  if (path == VNM_PATH_SMFMAC) return VNM_ERR_UNSUPPORTED;
   if (T == 0) return VNM_OK;
+  const bool matrix = packed && has_packed(V, M) && ldq % 16 == 0 && ((uintptr_t)Q & 15) == 0;
+  if (path == VNM_PATH_SMFMAC && !matrix) return VNM_ERR_UNSUPPORTED;
   (void)workspace;
   const I8Epilogue e{(const float*)scale_x, (const float*)scale_w, (const _Float16*)bias, Y, ldy, y_dtype};
+  if (path != VNM_PATH_GENERIC && matrix) return launch_spmm_i8_few(Q, T, ldq, packed, d, e, (hipStream_t)stream);
   return launch_spmm_i8_triple(Q, T, ldq, qvalues, meta, colidx, d, e, (hipStream_t)stream);
 }
