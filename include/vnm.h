@@ -379,9 +379,9 @@ typedef enum vnm_dtype { VNM_F16 = 0, VNM_F32 = 1, VNM_BF16 = 2 } vnm_dtype;
 
 /*
  * Activations to int8 with one scale per token:
- *   top[t] = max_i |X[t, i]|,  scale[t] = top[t] / 127,  Q[t, i] = rint(X[t, i] * f),  f = 127 / top[t]
- * in fp32, both quotients correctly rounded; the product with f is rounded once, to the integer (nearest,
- * ties to even), so that the result is defined to the bit.  |Q| <= 127.  A token whose top is below
+ *   top[t] = max_i |X[t, i]|,  scale[t] = top[t] * (1 / 127),  Q[t, i] = rint(X[t, i] * f),  f = (1 / top[t]) * 127
+ * in fp32, every quotient and product rounded to nearest by itself; the product with f is rounded once, to
+ * the integer (ties to even), so that the result is defined to the bit.  |Q| <= 127.  A token whose top is below
  * 2^-100 gets scale 0 and zeros; one that holds an infinity or a NaN gets scale NaN and zeros, and so
  * every result that is computed from it is NaN.
  *   X      dev [T x n] of type x_dtype (a vnm_dtype), leading dimension ldx >= n

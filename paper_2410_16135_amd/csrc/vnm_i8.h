@@ -37,6 +37,12 @@ inline I8Layout i8_layout(const Dims& d) {
   l.total = l.psel_off + up(rs * 64 * nt * i8_selectors(d.M)) + kI8Slack;
   return l;
 }
+// Staged activations: an image per (tile of kTokTile tokens, K step), 16 M rows [raw column][token] 160 bytes apart -- 8 rows that
+// differ modulo 8 then lie in 8 different eighths of the LDS banks --, padded to a multiple of 1 KiB.
+constexpr int kImagePitchI8 = kTokTile + 16;
+inline int64_t i8_image_bytes(int M) { return ((int64_t)16 * M * kImagePitchI8 + 1023) / 1024 * 1024; }
+int64_t staged_q_bytes(int64_t T, const Dims& d);
+
 // No sum may leave 32 bits, whatever the int8 values (-128 included)
 inline bool i8_sums_fit(const Dims& d) { return 2 * d.B <= (0x7FFFFFFFll >> 14); }
 
@@ -46,8 +52,10 @@ struct I8Epilogue {
   const float* scale_x; const float* scale_w; const _Float16* bias;
   void* Y; int64_t ldy; int y_dtype;
 };
-__device__ __forceinline__ float i8_result(int sum, float scale_w, float scale_x) {
-  return __fmul_rn(__fmul_rn((float)sum, scale_w), scale_x);
+__device__ __forceinline__ float i8_result(int sum, float scale_w, float scale_x, bool has_bias, float bias) {
+#pragma clang fp contract(off)
+  const float y = ((float)sum * scale_w) * scale_x;
+  return has_bias ? y + bias : y;
 }
 __device__ __forceinline__ unsigned short bf16_bits(float v) { return __builtin_bit_cast(unsigned short, (__bf16)v); }
 __device__ __forceinline__ void i8_store(const I8Epilogue& e, int64_t t, int64_t o, float v) {
@@ -59,9 +67,9 @@ __device__ __forceinline__ void i8_store(const I8Epilogue& e, int64_t t, int64_t
 // Quantization of a row to int8 (vnm_quantize_x): factor and scale from the largest magnitude.
 __device__ __forceinline__ void i8_factor(float top, float* factor, float* scale) {
   const bool bad = !(top < __builtin_inff());                       // an infinity, or a NaN
-  const bool none = top < 0x1p-100f;                                // 127 / top could leave fp32
-  *factor = bad || none ? 0.f : 127.f / top;
-  *scale = bad ? __builtin_nanf("") : none ? 0.f : top / 127.f;
+  const bool none = top < 0x1p-100f;                                // the quotient could leave fp32
+  *factor = bad || none ? 0.f : (1.f / top) * 127.f;
+  *scale = bad ? __builtin_nanf("") : none ? 0.f : top * (1.f / 127.f);
 }
 // x * factor rounded once to the integer: the addend's unit in the last place is 1 (fused, so the product is not rounded
 // before); the low byte of the sum's bits is the int8.  (factor 0: x may be infinite, the result is set to zero by the caller.)
@@ -79,6 +87,8 @@ int launch_quantize_rows(const void* X, int64_t T, int64_t n, int64_t ldx, int x
 int launch_pack_i8(const void* qvalues, const void* meta, const void* colidx, const Dims& d, void* packed, hipStream_t st);
 int launch_spmm_i8_triple(const void* Q, int64_t T, int64_t ldq, const void* qvalues, const void* meta, const void* colidx,
                           const Dims& d, const I8Epilogue& e, hipStream_t st);
+int launch_stage_q(const void* Q, int64_t T, int64_t ldq, const Dims& d, void* staged, hipStream_t st);
+int launch_spmm_i8_staged(const void* staged, int64_t T, const void* packed, const Dims& d, const I8Epilogue& e, hipStream_t st);
 int launch_spmm_i8_few(const void* Q, int64_t T, int64_t ldq, const void* packed, const Dims& d, const I8Epilogue& e, hipStream_t st);
 
 }  // namespace vnm

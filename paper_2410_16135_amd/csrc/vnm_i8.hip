@@ -1,5 +1,6 @@
 // The V:N:M layer in 8-bit integers: C entry points, the packed copy of an int8 weight, and the product on the canonical triple.
 #include "vnm_i8.h"
+#include "vnm_i8_rules.h"
 
 namespace vnm {
 
@@ -106,9 +107,7 @@ spmm_i8_triple_kernel(const signed char* __restrict__ Q, int64_t ldq, const sign
     if (c0 < in) acc += (int)v[2 * b] * x[c0];
     if (c1 < in) acc += (int)v[2 * b + 1] * x[c1];
   }
-  float y = i8_result(acc, e.scale_w[o], e.scale_x[t]);
-  if (e.bias) y = __fadd_rn(y, (float)e.bias[o]);
-  i8_store(e, t, o, y);
+  i8_store(e, t, o, i8_result(acc, e.scale_w[o], e.scale_x[t], e.bias, e.bias ? (float)e.bias[o] : 0.f));
 }
 
 int launch_spmm_i8_triple(const void* Q, int64_t T, int64_t ldq, const void* qvalues, const void* meta, const void* colidx,
@@ -162,7 +161,8 @@ extern "C" int vnm_spmm_i8_workspace_bytes(int64_t T, int64_t out, int64_t in, i
   if (!bytes) return VNM_ERR_NULL;
   if (int rc = check_pattern(out, in, V, N, M)) return rc;
   if (T < 0) return VNM_ERR_SHAPE;
-  *bytes = 0;
+  const Dims d = make_dims(out, in, V, M);
+  *bytes = has_packed(V, M) && T > 0 && !i8_takes_few(T, packed_row_blocks(d), in, i8_steps(d), M) ? staged_q_bytes(T, d) : 0;
   return VNM_OK;
 }
 
@@ -188,8 +188,13 @@ extern "C" int vnm_spmm_i8(const void* Q, int64_t T, int64_t ldq, const void* sc
   if (T == 0) return VNM_OK;
   const bool matrix = packed && has_packed(V, M) && ldq % 16 == 0 && ((uintptr_t)Q & 15) == 0;
   if (path == VNM_PATH_SMFMAC && !matrix) return VNM_ERR_UNSUPPORTED;
-  (void)workspace;
   const I8Epilogue e{(const float*)scale_x, (const float*)scale_w, (const _Float16*)bias, Y, ldy, y_dtype};
-  if (path != VNM_PATH_GENERIC && matrix) return launch_spmm_i8_few(Q, T, ldq, packed, d, e, (hipStream_t)stream);
+  if (path != VNM_PATH_GENERIC && matrix) {
+    if (i8_takes_few(T, packed_row_blocks(d), in, i8_steps(d), M)) return launch_spmm_i8_few(Q, T, ldq, packed, d, e, (hipStream_t)stream);
+    if (!workspace || workspace_bytes < staged_q_bytes(T, d)) return VNM_ERR_WORKSPACE;
+    if ((uintptr_t)workspace & 255) return VNM_ERR_ALIGN;
+    if (int rc = launch_stage_q(Q, T, ldq, d, workspace, (hipStream_t)stream)) return rc;
+    return launch_spmm_i8_staged(workspace, T, packed, d, e, (hipStream_t)stream);
+  }
   return launch_spmm_i8_triple(Q, T, ldq, qvalues, meta, colidx, d, e, (hipStream_t)stream);
 }

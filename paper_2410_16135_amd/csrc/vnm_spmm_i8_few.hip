@@ -1,8 +1,11 @@
 // Few tokens: the int8 product as a stream of the packed weight (vnm_spmm_i8).
 #include "vnm_i8.h"
+#include "vnm_i8_rules.h"
 
 namespace vnm {
 
+typedef unsigned u2v __attribute__((ext_vector_type(2)));
+typedef unsigned u4v __attribute__((ext_vector_type(4)));
 typedef int i4v __attribute__((ext_vector_type(4)));
 typedef int i8v __attribute__((ext_vector_type(8)));
 typedef int i16v __attribute__((ext_vector_type(16)));
@@ -17,7 +20,7 @@ struct I8FewArgs {
 // The 4 kept columns of the 8 blocks of a lane's run, from its raw dwords: a byte permutation per 8 bytes that a block can reach
 // into (selectors of bytes elsewhere give zero).
 template <int M>
-__device__ __forceinline__ i8v i8_gather(const unsigned (&x)[2 * M], const uint4* sel) {
+__device__ __forceinline__ i8v i8_gather(const unsigned (&x)[2 * M], const u4v* sel) {
   constexpr int NSEL = i8_selectors(M);
   i8v b;
 #pragma unroll
@@ -26,7 +29,7 @@ __device__ __forceinline__ i8v i8_gather(const unsigned (&x)[2 * M], const uint4
     unsigned v = 0;
 #pragma unroll
     for (int w = 0; w < NSEL; ++w) {
-      const unsigned s = ((const unsigned*)(sel + 2 * w))[d];
+      const unsigned s = sel[2 * w + (d >> 2)][d & 3];
       const int lo = first + 2 * w, hi = lo + 1;
       if (lo < 2 * M) {
         const unsigned p = __builtin_amdgcn_perm(hi < 2 * M ? x[hi] : 0u, x[lo], s);
@@ -38,114 +41,200 @@ __device__ __forceinline__ i8v i8_gather(const unsigned (&x)[2 * M], const uint4
   return b;
 }
 
-template <int M, int NT, int WAVES, int RING>
+// M: columns per block.  NT: column tables per 64-row block.  AT: 32-row tiles per workgroup (a row block's, or one of them).
+// TT: tokens per workgroup.  WAVES: they cut the K steps between them, a contiguous run each.
+template <int M, int NT, int AT, int TT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES)
 spmm_i8_few_kernel(const I8FewArgs a, const int tp) {
-  extern __shared__ __attribute__((aligned(16))) int red[];       // [wave][row][tp tokens]
-  constexpr int NSEL = i8_selectors(M);
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  constexpr int NSEL = i8_selectors(M), G = (TT + 31) / 32, TABLES = AT == 2 ? NT : 1;
+  constexpr int CS = M <= 8 ? 2 : 1;               // K steps of a chunk of activations
+  constexpr int PIECES = CS * M;                   // its 16-byte pieces per token
+  constexpr int PITCH = PIECES * 16 + (M % 2 ? 8 : 16);   // 2 or 4 times an odd number of dwords: the lanes' reads below cover all banks
+  constexpr int NX = (TT * PIECES + 63) / 64;      // pieces per lane
+  constexpr int RC = 2;                            // chunks of weights that a wave requests ahead
   const int lane = threadIdx.x & 63, j = lane & 31, h = lane >> 5;
   const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned n = blockIdx.x;
-  // both tiles of a row block on one XCD (workgroup n runs on XCD n mod 8): they share the positions' and selectors' lines
-  const bool by_xcd = n < (gridDim.x & ~15u);
-  const unsigned at = by_xcd ? (n >> 3) & 1 : n & 1, rp = by_xcd ? (n >> 4) * 8 + (n & 7) : n >> 1;
-  const int64_t t0 = (int64_t)blockIdx.y * 32;
-  const int nt = a.T - t0 < 32 ? (int)(a.T - t0) : 32;
-  const unsigned char* xrow = a.Q + (t0 + (j < nt ? j : nt - 1)) * a.ldq;
-  const unsigned S = a.S;
+  unsigned at = 0, rp = n;
+  if (AT == 1) {
+    // both tiles of a row block on one XCD (workgroup n runs on XCD n mod 8): they share the positions' and selectors' lines
+    const bool by_xcd = n < (gridDim.x & ~15u);
+    at = by_xcd ? (n >> 3) & 1 : n & 1;
+    rp = by_xcd ? (n >> 4) * 8 + (n & 7) : n >> 1;
+  }
+  const int64_t t0 = (int64_t)blockIdx.y * TT;
+  const int nt = a.T - t0 < TT ? (int)(a.T - t0) : TT;
+  const unsigned S = a.S, per = (S + WAVES - 1) / WAVES;
+  const unsigned s0 = wave * per < S ? wave * per : S, s1 = s0 + per < S ? s0 + per : S;
   const size_t rs0 = (size_t)rp * S;
+  unsigned char* const xs = smem + wave * (TT * PITCH);        // this wave's activations: [token][a chunk's raw columns]
 
-  struct Slot { uint4 w; unsigned idx; uint4 sel[2 * NSEL]; unsigned x[2 * M]; };
-  auto load = [&](Slot& o, unsigned s) {
-    s = s < S ? s : S - 1;                         // (beyond the range: not used)
+  // addresses as a uniform base and a 32-bit offset of the lane
+  const unsigned char* const xbase = a.Q + t0 * a.ldq;
+  unsigned xrow[NX], xcol[NX], xdst[NX];
+#pragma unroll
+  for (int i = 0; i < NX; ++i) {
+    int q = i * 64 + lane;
+    if (q >= TT * PIECES) q = TT * PIECES - 1;
+    const int tok = q / PIECES, piece = q - tok * PIECES;
+    xrow[i] = (unsigned)(tok < nt ? tok : nt - 1) * (unsigned)a.ldq;
+    xcol[i] = piece * 16;
+    xdst[i] = tok * PITCH + piece * 16;
+  }
+  u4v xr[NX];
+  // A piece that begins inside the row is read whole: it is aligned, so what it holds past the row's end stands in the same
+  // 16 bytes as the row's last channel.  Columns past the end meet weights that are zero.
+  auto load_x = [&](unsigned s) {
+#pragma unroll
+    for (int i = 0; i < NX; ++i) {
+      const unsigned c = s * (16 * M) + xcol[i];
+      xr[i] = *(const u4v*)(xbase + (xrow[i] + (c < (unsigned)a.in ? c : 0u)));
+    }
+  };
+  auto store_x = [&]() {
+#pragma unroll
+    for (int i = 0; i < NX; ++i) {
+      if constexpr (M % 2 == 0) *(u4v*)(xs + xdst[i]) = xr[i];
+      else {
+        *(u2v*)(xs + xdst[i]) = xr[i].xy;
+        *(u2v*)(xs + xdst[i] + 8) = xr[i].zw;
+      }
+    }
+  };
+  struct Slot { u4v w[AT]; unsigned idx[AT]; u4v sel[TABLES * 2 * NSEL]; };
+  auto load_w = [&](Slot& o, unsigned s) {
+    s = s < S ? s : S - 1;                         // (beyond the wave's range: not used)
     const size_t rs = rs0 + s;
-    o.w = *(const uint4*)(a.pa + (rs * 2 + at) * 1024 + lane * 16);
-    o.idx = *(const unsigned*)(a.pidx + rs * 512 + lane * 8 + at * 4);
 #pragma unroll
-    for (int k = 0; k < NSEL; ++k)
+    for (int i = 0; i < AT; ++i) o.w[i] = *(const u4v*)(a.pa + (rs * 2 + (AT == 2 ? i : at)) * 1024 + (unsigned)(lane * 16));
+    if constexpr (AT == 2) {
+      const u2v v = *(const u2v*)(a.pidx + rs * 512 + (unsigned)(lane * 8));
+      o.idx[0] = v.x; o.idx[1] = v.y;
+    } else o.idx[0] = *(const unsigned*)(a.pidx + rs * 512 + at * 4 + (unsigned)(lane * 8));
 #pragma unroll
-      for (int q = 0; q < 2; ++q)
-        o.sel[2 * k + q] = *(const uint4*)(a.psel + ((rs * NT + (NT == 2 ? at : 0)) * NSEL + k) * 64 + h * 32 + q * 16);
-    const int col = (int)(s * 16 * M) + 8 * M * h;
-    // A piece that begins inside the row is read whole: it is aligned, so what it holds past the row's end stands in the same
-    // 16 bytes as the row's last channel.  A piece past the end meets weights that are zero.
-    if constexpr (M % 2 == 0) {
+    for (int t = 0; t < TABLES; ++t)
 #pragma unroll
-      for (int k = 0; k < M / 2; ++k) {
-        const int c = col + 16 * k;
-        const uint4 v = *(const uint4*)(xrow + (c < a.in ? c : 0));
-        o.x[4 * k] = v.x; o.x[4 * k + 1] = v.y; o.x[4 * k + 2] = v.z; o.x[4 * k + 3] = v.w;
+      for (int k = 0; k < NSEL; ++k)
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          o.sel[(t * NSEL + k) * 2 + q] =
+              *(const u4v*)(a.psel + ((rs * NT + (AT == 2 ? t : NT == 2 ? at : 0)) * NSEL + k) * 64 + q * 16 + (unsigned)(h * 32));
+  };
+  i16v acc[AT][G];
+#pragma unroll
+  for (int i = 0; i < AT; ++i)
+#pragma unroll
+    for (int g = 0; g < G; ++g) acc[i][g] = (i16v)0;
+  auto multiply = [&](const Slot& o, int sl) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int tok = g * 32 + j < TT ? g * 32 + j : TT - 1;
+      const unsigned char* p = xs + tok * PITCH + sl * (16 * M) + h * (8 * M);
+      unsigned x[2 * M];
+      if constexpr (M % 2 == 0) {
+#pragma unroll
+        for (int k = 0; k < M / 2; ++k) {
+          const u4v v = *(const u4v*)(p + 16 * k);
+          x[4 * k] = v.x; x[4 * k + 1] = v.y; x[4 * k + 2] = v.z; x[4 * k + 3] = v.w;
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < M; ++k) {
+          const u2v v = *(const u2v*)(p + 8 * k);
+          x[2 * k] = v.x; x[2 * k + 1] = v.y;
+        }
       }
-    } else {
+      i8v b = i8_gather<M>(x, o.sel);
 #pragma unroll
-      for (int k = 0; k < M; ++k) {
-        const int c = col + 8 * k;
-        const uint2 v = *(const uint2*)(xrow + (c < a.in ? c : 0));
-        o.x[2 * k] = v.x; o.x[2 * k + 1] = v.y;
+      for (int i = 0; i < AT; ++i) {
+        if (TABLES == 2 && i == 1) b = i8_gather<M>(x, o.sel + 2 * NSEL);
+        acc[i][g] = __builtin_amdgcn_smfmac_i32_32x32x64_i8(__builtin_bit_cast(i4v, o.w[i]), b, acc[i][g], (int)o.idx[i], 0, 0);
       }
     }
   };
-  Slot ring[RING];
-  i16v acc = {};
-  auto multiply = [&](const Slot& o) {
-    const i8v b = i8_gather<M>(o.x, o.sel);
-    acc = __builtin_amdgcn_smfmac_i32_32x32x64_i8(__builtin_bit_cast(i4v, o.w), b, acc, (int)o.idx, 0, 0);
-  };
+  Slot ring[RC][CS];
+  load_x(s0);
 #pragma unroll
-  for (int i = 0; i < RING; ++i) load(ring[i], wave + i * WAVES);
-  for (unsigned sb = wave; sb < S; sb += RING * WAVES) {
-    if (sb + RING * WAVES < S) {
+  for (int c = 0; c < RC; ++c)
 #pragma unroll
-      for (int i = 0; i < RING; ++i) {
-        multiply(ring[i]);                         // (sb + i * WAVES < S, as the round after this one exists)
-        load(ring[i], sb + (RING + i) * WAVES);
+    for (int k = 0; k < CS; ++k) load_w(ring[c][k], s0 + c * CS + k);
+  for (unsigned sb = s0; sb < s1; sb += RC * CS) {
+#pragma unroll
+    for (int c = 0; c < RC; ++c) {
+      const unsigned sc = sb + c * CS;
+      if (sc >= s1) break;
+      // The chunk's activations go through LDS, where each lane finds the run of its token.  The region is the wave's own and
+      // LDS executes a wave's accesses in order; the fences keep the compiler from moving reads and writes past each other.
+      __builtin_amdgcn_wave_barrier();
+      store_x();
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      load_x(sc + CS);
+#pragma unroll
+      for (int k = 0; k < CS; ++k) {
+        if (sc + k < s1) multiply(ring[c][k], k);
+        load_w(ring[c][k], sc + RC * CS + k);
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < RING; ++i)
-        if (sb + i * WAVES < S) multiply(ring[i]);
     }
   }
-  if (j < nt) {
+  __syncthreads();                                 // the sums take the place of the activations
+  int* red = (int*)smem;                           // [wave][row][tp]
 #pragma unroll
-    for (int r = 0; r < 16; ++r) red[(wave * 32 + 8 * (r >> 2) + 4 * h + (r & 3)) * tp + j] = acc[r];
-  }
+  for (int g = 0; g < G; ++g)
+    if (g * 32 + j < nt) {
+#pragma unroll
+      for (int i = 0; i < AT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          red[(wave * (32 * AT) + i * 32 + 8 * (r >> 2) + 4 * h + (r & 3)) * tp + g * 32 + j] = acc[i][g][r];
+    }
   __syncthreads();
-  for (int k = threadIdx.x; k < 32 * nt; k += 64 * WAVES) {
-    const int row = k & 31, tok = k >> 5;
+  for (int k = threadIdx.x; k < 32 * AT * nt; k += 64 * WAVES) {
+    const int row = k % (32 * AT), tok = k / (32 * AT);
     const int64_t o = (int64_t)rp * 64 + at * 32 + row, t = t0 + tok;
     if (o >= a.out) continue;
     int sum = 0;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) sum += red[(w * 32 + row) * tp + tok];
-    float y = i8_result(sum, a.e.scale_w[o], a.e.scale_x[t]);
-    if (a.e.bias) y = __fadd_rn(y, (float)a.e.bias[o]);
-    i8_store(a.e, t, o, y);
+    for (int w = 0; w < WAVES; ++w) sum += red[(w * (32 * AT) + row) * tp + tok];
+    i8_store(a.e, t, o, i8_result(sum, a.e.scale_w[o], a.e.scale_x[t], a.e.bias, a.e.bias ? (float)a.e.bias[o] : 0.f));
   }
 }
 
-template <int M, int NT, int WAVES>
+template <int M, int NT, int AT, int TT, int WAVES>
 static int launch_few_cfg(const I8FewArgs& a, int64_t R64, hipStream_t st) {
-  constexpr int RING = M <= 5 ? 4 : M <= 8 ? 3 : 2;
-  auto kern = spmm_i8_few_kernel<M, NT, WAVES, RING>;
+  constexpr int CS = M <= 8 ? 2 : 1, PITCH = CS * M * 16 + (M % 2 ? 8 : 16);
+  auto kern = spmm_i8_few_kernel<M, NT, AT, TT, WAVES>;
   if (int rc = allow_big_lds((const void*)kern, "hipFuncSetAttribute(spmm_i8_few)")) return rc;
-  const int tp = (int)(a.T < 32 ? a.T : 32) | 1;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(2 * R64), (unsigned)((a.T + 31) / 32)), dim3(64 * WAVES), (size_t)WAVES * 32 * tp * 4, st, a, tp);
+  const int tp = (int)(a.T < TT ? a.T : TT) | 1;
+  const size_t xs = (size_t)WAVES * TT * PITCH, sums = (size_t)WAVES * 32 * AT * tp * 4;
+  static_assert((size_t)WAVES * TT * PITCH <= 160 * 1024 && (size_t)WAVES * 32 * AT * (TT | 1) * 4 <= 160 * 1024, "LDS of a compute unit");
+  hipLaunchKernelGGL(kern, dim3((unsigned)(AT == 1 ? 2 * R64 : R64), (unsigned)((a.T + TT - 1) / TT)), dim3(64 * WAVES), xs > sums ? xs : sums, st, a, tp);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) { set_hip_error(e, "spmm_i8_few_kernel"); return VNM_ERR_HIP; }
   return VNM_OK;
 }
-template <int M>
+template <int M, int NT>
 static int launch_few_m(const I8FewArgs& a, const Dims& d, hipStream_t st) {
   const int64_t R64 = packed_row_blocks(d);
-  if (packed_tables(d.V) == 2) return a.S > 8 ? launch_few_cfg<M, 2, 16>(a, R64, st) : launch_few_cfg<M, 2, 4>(a, R64, st);
-  return a.S > 8 ? launch_few_cfg<M, 1, 16>(a, R64, st) : launch_few_cfg<M, 1, 4>(a, R64, st);
+  const I8FewShape s = i8_few_shape(a.T, R64, a.S, M);
+  if (s.tiles == 2) return launch_few_cfg<M, NT, 2, 32, 4>(a, R64, st);
+  if (s.waves == 8)
+    return s.tokens == 4 ? launch_few_cfg<M, NT, 1, 4, 8>(a, R64, st) : s.tokens == 16 ? launch_few_cfg<M, NT, 1, 16, 8>(a, R64, st)
+                                                                       : launch_few_cfg<M, NT, 1, 32, 8>(a, R64, st);
+  return s.tokens == 4 ? launch_few_cfg<M, NT, 1, 4, 4>(a, R64, st) : s.tokens == 16 ? launch_few_cfg<M, NT, 1, 16, 4>(a, R64, st)
+                                                                     : launch_few_cfg<M, NT, 1, 32, 4>(a, R64, st);
+}
+template <int M>
+static int launch_few_m(const I8FewArgs& a, const Dims& d, hipStream_t st) {
+  return packed_tables(d.V) == 2 ? launch_few_m<M, 2>(a, d, st) : launch_few_m<M, 1>(a, d, st);
 }
 
 int launch_spmm_i8_few(const void* Q, int64_t T, int64_t ldq, const void* packed, const Dims& d, const I8Epilogue& e, hipStream_t st) {
   const I8Layout l = i8_layout(d);
   const unsigned char* p = (const unsigned char*)packed;
-  if (2 * packed_row_blocks(d) > 0x7FFFFFFF || (T + 31) / 32 > 65535 || i8_steps(d) * 16 * d.M > 0x7FFFFFFF) return VNM_ERR_UNSUPPORTED;
+  if (2 * packed_row_blocks(d) > 0x7FFFFFFF || (T + 3) / 4 > 65535 || i8_steps(d) * 16 * d.M > 0x7FFFFFFF || 64 * ldq + i8_steps(d) * 16 * d.M > 0x7FFFFFFF) return VNM_ERR_UNSUPPORTED;
   const I8FewArgs a{(const unsigned char*)Q, T, ldq, (int)d.in, p, p + l.pidx_off, p + l.psel_off, d.out, (unsigned)i8_steps(d), e};
   switch (d.M) {
     case 4: return launch_few_m<4>(a, d, st);

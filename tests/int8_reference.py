@@ -14,8 +14,8 @@ def quantize_rows(x):
     bad = ~(top < np.inf)
     none = top < np.float32(2.0 ** -100)
     with np.errstate(all="ignore"):
-        factor = np.where(bad | none, np.float32(0), np.float32(127) / top).astype(np.float32)
-        scale = np.where(bad, np.float32(np.nan), np.where(none, np.float32(0), top / np.float32(127))).astype(np.float32)
+        factor = np.where(bad | none, np.float32(0), (np.float32(1) / top) * np.float32(127)).astype(np.float32)
+        scale = np.where(bad, np.float32(np.nan), np.where(none, np.float32(0), top * (np.float32(1) / np.float32(127)))).astype(np.float32)
         q = np.rint(x.astype(np.float64) * factor.astype(np.float64)[:, None])
     q[bad | none] = 0
     return q.astype(np.int8), scale
