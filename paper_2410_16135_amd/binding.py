@@ -5,6 +5,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 from dataclasses import dataclass
 from typing import NamedTuple
 
@@ -41,6 +42,12 @@ _ResidualNormBackwardArgs = _struct(
     (_I64, "gate_tokens"), (_PTR, "dx dh_out h_new y gate post_weight post_bias pre_weight stats"),
     (_I64, "lddx lddho ldh ldy ldg"), (_PTR, "dh dy d_post_weight d_post_bias d_pre_weight d_pre_bias d_gate"),
     (_I64, "lddh lddy"))
+
+
+# The same bytes from struct.pack, which a call on few tokens builds in a third of the time
+_NORM_ARGS = struct.Struct("@2q4i3f4xq" + "7P3q" + "5P3q")
+_NORM_BACKWARD_ARGS = struct.Struct("@2q4if4xq" + "9P5q" + "7P2q")
+assert _NORM_ARGS.size == ctypes.sizeof(_ResidualNormArgs) and _NORM_BACKWARD_ARGS.size == ctypes.sizeof(_ResidualNormBackwardArgs)
 
 
 def lib_path() -> str:
@@ -133,8 +140,8 @@ def load_library():
     lib.vnm_pack_i8.argtypes = [vp, vp, vp, i64, i64, ci, ci, ci, vp, vp]
     lib.vnm_spmm_i8.argtypes = [vp, i64, i64, vp, vp, vp, vp, vp, vp, i64, i64, ci, ci, ci, vp, vp, i64, ci, ci, vp, i64, vp]
     lib.vnm_spmm_i8_workspace_bytes.argtypes = [i64, i64, i64, ci, ci, ci, ctypes.POINTER(i64)]
-    lib.vnm_residual_norm.argtypes = [ctypes.POINTER(_ResidualNormArgs), vp]
-    lib.vnm_residual_norm_backward.argtypes = [ctypes.POINTER(_ResidualNormBackwardArgs), vp, i64, vp]
+    lib.vnm_residual_norm.argtypes = [vp, vp]
+    lib.vnm_residual_norm_backward.argtypes = [vp, vp, i64, vp]
     lib.vnm_residual_norm_backward_workspace_bytes.argtypes = [i64, i64, i64, ctypes.POINTER(i64)]
     for f in (lib.vnm_quantize_x, lib.vnm_i8_packed_bytes, lib.vnm_quantize_compressed, lib.vnm_pack_i8, lib.vnm_spmm_i8,
               lib.vnm_spmm_i8_workspace_bytes, lib.vnm_residual_norm, lib.vnm_residual_norm_backward,
@@ -625,12 +632,20 @@ def _dtype_code(dtype) -> int:
     return code
 
 
+def _current_device() -> int:
+    """The current CUDA device (torch's own query without its checks for a first use)."""
+    global _current_device
+    import torch
+    _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _current_device()
+
+
 def _launch(what: str, fn, device, *args):
     """fn(*args, stream) on the device's current stream, with that device current."""
-    import torch
-    if torch.cuda.current_device() == device.index:
+    if _current_device() == device.index:
         status = fn(*args, _raw_stream(device))
     else:
+        import torch
         with torch.cuda.device(device):
             status = fn(*args, _raw_stream(device))
     if status:
@@ -639,17 +654,20 @@ def _launch(what: str, fn, device, *args):
 
 def _rows(name, t, T, n, device, dtype=None):
     """Checks a [T x n] tensor with rows of consecutive elements; returns its leading dimension."""
-    assert t.device == device and t.dim() == 2 and t.shape[0] == T and t.shape[1] == n, name
-    assert dtype is None or t.dtype == dtype, name
+    assert t.shape == (T, n) and (dtype is None or t.dtype == dtype) and t.device == device, name
+    if T > 1:
+        ld, one = t.stride()
+        assert ld >= n and (one == 1 or n == 1), name
+        return ld
     assert T == 0 or n == 1 or t.stride(1) == 1, name
-    ld = t.stride(0) if T > 1 else n
-    assert T <= 1 or ld >= n, name
-    return ld
+    return n
 
 
 def _vector(name, t, n, device, dtype):
-    assert t is None or (t.device == device and t.dtype == dtype and t.shape == (n,) and t.is_contiguous()), name
-    return 0 if t is None else t.data_ptr()
+    if t is None:
+        return 0
+    assert t.shape == (n,) and t.dtype == dtype and t.device == device and t.is_contiguous(), name
+    return t.data_ptr()
 
 
 def _empty_i8_rows(T: int, n: int, device):
@@ -662,19 +680,22 @@ def _empty_i8_rows(T: int, n: int, device):
 
 def vnm_quantize_x(X, Q=None, scale=None):
     """int8 activations with one scale per token: (Q int8 [T x n], scale fp32 [T]) of X [T x n] (fp16, bf16 or fp32),
-    Q = rint(X * (127 / max|X_t|)), scale = max|X_t| / 127.  A fresh Q has rows 16 bytes aligned."""
+    Q = rint(X * ((1 / max|X_t|) * 127)), scale = max|X_t| * (1 / 127).  A fresh Q has rows 16 bytes aligned."""
     import torch
     assert X.is_cuda and X.dim() == 2
     T, n = X.shape
     dev = X.device
     ldx = _rows("X", X, T, n, dev)
     if Q is None:
-        Q = _empty_i8_rows(T, n, dev)
+        Q, ldq = _empty_i8_rows(T, n, dev), (n + 15) // 16 * 16
+    else:
+        ldq = _rows("Q", Q, T, n, dev, torch.int8)
     if scale is None:
         scale = torch.empty(T, dtype=torch.float32, device=dev)
-    ldq = _rows("Q", Q, T, n, dev, torch.int8)
+    else:
+        _vector("scale", scale, T, dev, torch.float32)
     _launch("vnm_quantize_x", load_library().vnm_quantize_x, dev, X.data_ptr(), T, n, ldx, _dtype_code(X.dtype), Q.data_ptr(),
-            ldq, _vector("scale", scale, T, dev, torch.float32))
+            ldq, scale.data_ptr())
     return Q, scale
 
 
@@ -752,19 +773,23 @@ def vnm_spmm_i8(Q, scale, c: CompressedI8, bias=None, N: int = 2, out_dtype=None
     import torch
     assert Q.is_cuda and Q.dim() == 2
     T, dev = Q.shape[0], Q.device
-    ldq = _rows("Q", Q, T, c.inn, dev, torch.int8)
+    out, inn, values = c.out, c.inn, c.values
+    ldq = _rows("Q", Q, T, inn, dev, torch.int8)
     if T == 1:
-        ldq = (c.inn + 15) // 16 * 16            # (one row: whatever the view's stride)
-    assert c.values.device == dev and c.scale.device == dev
+        ldq = (inn + 15) // 16 * 16              # (one row: whatever the view's stride)
+    assert values.device == dev
     if Y is None:
-        Y = torch.empty((T, c.out), dtype=out_dtype or torch.float16, device=dev)
-    ldy = _rows("Y", Y, T, c.out, dev)
-    need = 0 if path == PATH_GENERIC or c.packed is None else _spmm_i8_workspace_bytes(T, c.out, c.inn, c.V, N, c.M)
-    if need and workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        Y, ldy = torch.empty((T, out), dtype=out_dtype or torch.float16, device=dev), out
+    else:
+        ldy = _rows("Y", Y, T, out, dev)
+    packed = c.packed
+    if workspace is None and packed is not None and path != PATH_GENERIC:
+        need = _spmm_i8_workspace_bytes(T, out, inn, c.V, N, c.M)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     _launch("vnm_spmm_i8", load_library().vnm_spmm_i8, dev, Q.data_ptr(), T, ldq, _vector("scale", scale, T, dev, torch.float32),
-            _ptr(c.values), _ptr(c.meta), _ptr(c.colidx), _ptr(c.packed), _vector("c.scale", c.scale, c.out, dev, torch.float32),
-            c.out, c.inn, c.V, N, c.M, _vector("bias", bias, c.out, dev, torch.float16), Y.data_ptr(), ldy, _dtype_code(Y.dtype),
+            values.data_ptr(), c.meta.data_ptr(), c.colidx.data_ptr(), _ptr(packed), _vector("c.scale", c.scale, out, dev, torch.float32),
+            out, inn, c.V, N, c.M, _vector("bias", bias, out, dev, torch.float16), Y.data_ptr(), ldy, _dtype_code(Y.dtype),
             path, _ptr(workspace), 0 if workspace is None else workspace.numel())
     return Y
 
@@ -824,8 +849,9 @@ def vnm_residual_norm(h, y=None, gate=None, gate_tokens: int = 0, residual_scale
     T, n, dev, xt, ldh, ldy, ldg = _norm_operands(h, y, gate, gate_tokens, post, pre, x_dtype,
                                                   (post_weight, post_bias, pre_weight, pre_bias))
     if h_out is None:
-        h_out = torch.empty((T, n), dtype=h.dtype, device=dev)
-    ldho = _rows("h_out", h_out, T, n, dev, h.dtype)
+        h_out, ldho = torch.empty((T, n), dtype=h.dtype, device=dev), n
+    else:
+        ldho = _rows("h_out", h_out, T, n, dev, h.dtype)
     x = q = scale = stats = None
     if want_x and int8:
         q, scale = _empty_i8_rows(T, n, dev), torch.empty(T, dtype=torch.float32, device=dev)
@@ -833,12 +859,12 @@ def vnm_residual_norm(h, y=None, gate=None, gate_tokens: int = 0, residual_scale
         x = torch.empty((T, n), dtype=xt, device=dev)
     if want_stats:
         stats = torch.empty((T, 4), dtype=torch.float32, device=dev)
-    a = _ResidualNormArgs(
+    a = _NORM_ARGS.pack(
         T, n, _dtype_code(h.dtype), _dtype_code(xt), _NORMS[post], _NORMS[pre], post_eps, pre_eps, residual_scale, gate_tokens,
         h.data_ptr(), _ptr(y), _ptr(gate), _vector("post_weight", post_weight, n, dev, xt), _vector("post_bias", post_bias, n, dev, xt),
         _vector("pre_weight", pre_weight, n, dev, xt), _vector("pre_bias", pre_bias, n, dev, xt), ldh, ldy, ldg,
         h_out.data_ptr(), _ptr(x), _ptr(q), _ptr(scale), _ptr(stats), ldho, n, (n + 15) // 16 * 16)
-    _launch("vnm_residual_norm", load_library().vnm_residual_norm, dev, ctypes.byref(a))
+    _launch("vnm_residual_norm", load_library().vnm_residual_norm, dev, a)
     return ResidualNorm(h_out, q if int8 else x, scale, stats)
 
 
@@ -848,32 +874,40 @@ def vnm_residual_norm_backward(h, stats, dx=None, dh=None, y=None, gate=None, ga
                                workspace=None) -> ResidualNormGrads:
     """Gradients of vnm_residual_norm from dx and dh, those of its results x and h (either may be None).  `h` and `stats` are
     what the forward call returned (its h, with want_stats), everything else what it was given.  Sums over the tokens (weights,
-    biases, gate) come in fp32; the gradient of an argument that is None is None."""
+    biases, gate) come in fp32; the gradient of an argument that is None is None, and without dx those of the pre norm's are too."""
     import torch
     T, n, dev, xt, ldh, ldy, ldg = _norm_operands(h, y, gate, gate_tokens, post, pre, None if dx is None else dx.dtype,
                                                   (post_weight, post_bias, pre_weight, pre_bias, gate))
     lddx = 0 if dx is None else _rows("dx", dx, T, n, dev, xt)
     lddho = 0 if dh is None else _rows("dh", dh, T, n, dev, h.dtype)
     assert stats is None or (stats.shape == (T, 4) and stats.dtype == torch.float32 and stats.is_contiguous() and stats.device == dev)
-    empty = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=dev)
-    gh = empty((T, n), h.dtype) if want_dh else None
-    gy = empty((T, n), xt) if want_dy and y is not None else None
-    vec = lambda t: empty((n,), torch.float32) if want_params and t is not None else None
-    g_pw, g_pb = vec(pre_weight) if dx is not None else None, vec(pre_bias) if dx is not None else None
-    g_ow, g_ob = vec(post_weight), vec(post_bias)
-    g_gate = empty(gate.shape, torch.float32) if want_params and gate is not None else None
-    lib = load_library()
-    if workspace is None and any(t is not None for t in (g_pw, g_pb, g_ow, g_ob, g_gate)):
-        b = ctypes.c_int64(0)
-        _check(lib.vnm_residual_norm_backward_workspace_bytes(T, n, gate_tokens if gate is not None else 0, ctypes.byref(b)),
-               "vnm_residual_norm_backward_workspace_bytes")
-        workspace = torch.empty(b.value, dtype=torch.uint8, device=dev)
-    a = _ResidualNormBackwardArgs(
-        T, n, _dtype_code(h.dtype), _dtype_code(xt), _NORMS[post], _NORMS[pre], residual_scale, gate_tokens if gate is not None else 0,
+    gh = torch.empty((T, n), dtype=h.dtype, device=dev) if want_dh else None
+    gy = torch.empty((T, n), dtype=xt, device=dev) if want_dy and y is not None else None
+    _vector("pre_bias", pre_bias, n, dev, xt)
+    g_gate = g_ow = g_ob = g_pw = g_pb = None
+    lib, tokens = load_library(), gate_tokens if gate is not None else 0
+    if want_params:
+        g_gate = torch.empty(gate.shape, dtype=torch.float32, device=dev) if gate is not None else None
+        through = (post_weight, post_bias) + ((pre_weight, pre_bias) if dx is not None else (None, None))
+        count = sum(t is not None for t in through)
+        if count:
+            rows = iter(torch.empty((count, n), dtype=torch.float32, device=dev).unbind(0))
+            g_ow, g_ob, g_pw, g_pb = (None if t is None else next(rows) for t in through)
+        if workspace is None and (count or gate is not None):
+            workspace = torch.empty(_backward_workspace_bytes(T, n, tokens), dtype=torch.uint8, device=dev)
+    a = _NORM_BACKWARD_ARGS.pack(
+        T, n, _dtype_code(h.dtype), _dtype_code(xt), _NORMS[post], _NORMS[pre], residual_scale, tokens,
         _ptr(dx), _ptr(dh), h.data_ptr(), _ptr(y), _ptr(gate), _vector("post_weight", post_weight, n, dev, xt),
         _vector("post_bias", post_bias, n, dev, xt), _vector("pre_weight", pre_weight, n, dev, xt), _ptr(stats), lddx, lddho, ldh, ldy,
         ldg, _ptr(gh), _ptr(gy), _ptr(g_ow), _ptr(g_ob), _ptr(g_pw), _ptr(g_pb), _ptr(g_gate), n, n)
-    _vector("pre_bias", pre_bias, n, dev, xt)
-    _launch("vnm_residual_norm_backward", lib.vnm_residual_norm_backward, dev, ctypes.byref(a), _ptr(workspace),
+    _launch("vnm_residual_norm_backward", lib.vnm_residual_norm_backward, dev, a, _ptr(workspace),
             0 if workspace is None else workspace.numel())
     return ResidualNormGrads(gh, gy, g_gate, g_ow, g_ob, g_pw, g_pb)
+
+
+@functools.lru_cache(maxsize=1024, typed=True)      # (typed: 16.0 is refused, also after 16)
+def _backward_workspace_bytes(T: int, n: int, gate_tokens: int) -> int:
+    b = ctypes.c_int64(0)
+    _check(load_library().vnm_residual_norm_backward_workspace_bytes(T, n, gate_tokens, ctypes.byref(b)),
+           "vnm_residual_norm_backward_workspace_bytes")
+    return b.value

@@ -44,15 +44,22 @@ __device__ __forceinline__ void store_row(T* p, int n, int tid, bool vec, const 
   }
 }
 
+// Over a wave by the data-parallel shifts of its rows of 16 lanes and two broadcasts, which need no LDS; the result, taken from
+// the last lane, is uniform.  Lanes without a source add 0.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned dpp(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false); }
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-  return v;
+  auto add = [&](unsigned o) { v += __builtin_bit_cast(float, o); };
+  const auto bits = [&] { return __builtin_bit_cast(unsigned, v); };
+  add(dpp<0x111, 0xf>(bits())); add(dpp<0x112, 0xf>(bits())); add(dpp<0x114, 0xf>(bits())); add(dpp<0x118, 0xf>(bits()));
+  add(dpp<0x142, 0xa>(bits())); add(dpp<0x143, 0xc>(bits()));
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane((int)bits(), 63));
 }
 __device__ __forceinline__ unsigned wave_max(unsigned v) {
-#pragma unroll
-  for (int m = 32; m; m >>= 1) { const unsigned w = __shfl_xor(v, m); v = w > v ? w : v; }
-  return v;
+  auto top = [&](unsigned o) { v = o > v ? o : v; };
+  top(dpp<0x111, 0xf>(v)); top(dpp<0x112, 0xf>(v)); top(dpp<0x114, 0xf>(v)); top(dpp<0x118, 0xf>(v));
+  top(dpp<0x142, 0xa>(v)); top(dpp<0x143, 0xc>(v));
+  return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
 }
 // Over the TPR threads that share a row.  `lds`: two halves of TPR / 64 pairs, used in turn (`turn`), so that one barrier per
 // reduction is enough: a wave reaches the use after next of a half only past the barrier of the next.

@@ -10,9 +10,9 @@
 namespace vnm {
 
 template <typename HT, typename XT, int TPR, int NCH>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
+__global__ void __launch_bounds__(TPR == 64 ? 256 : TPR)
 residual_norm_kernel(const vnm_residual_norm_args a, const int64_t scale_rows, const int vec) {
-  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;         // rows that a workgroup has at a time
+  constexpr int RPB = TPR == 64 ? 4 : 1;         // rows that a workgroup has at a time
   __shared__ float2 lds[TPR == 64 ? 1 : 2 * (TPR / 64)];
   int turn = 0;
   const int tid = TPR == 64 ? (threadIdx.x & 63) : threadIdx.x;
@@ -58,35 +58,48 @@ residual_norm_kernel(const vnm_residual_norm_args a, const int64_t scale_rows, c
       }
   };
 
-  for (int64_t t = (int64_t)blockIdx.x * RPB + (TPR == 64 ? threadIdx.x >> 6 : 0); t < a.T; t += (int64_t)gridDim.x * RPB) {
-    Octet<HT> hr[NCH];
-    Octet<XT> yr[NCH];
+  // The next row is requested when this one's has been taken over into fp32: its way from memory overlaps the reductions.
+  Octet<HT> hr[NCH];
+  Octet<XT> yr[NCH];
+  auto request = [&](int64_t t) {
     load_row<HT, TPR, NCH>((const HT*)a.h + t * a.ldh, n, tid, vec, hr);
     if (a.y) load_row<XT, TPR, NCH>((const XT*)a.y + t * a.ldy, n, tid, vec, yr);
+  };
+  const int64_t first = (int64_t)blockIdx.x * RPB + (TPR == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
+  const int64_t stride = (int64_t)gridDim.x * RPB;
+  if (first < a.T) request(first);
+  for (int64_t t = first; t < a.T; t += stride) {
     if (a.gate) {
       const int64_t g = a.gate_tokens ? t / a.gate_tokens : 0;
       if (g != gate_at) load_row<XT, TPR, NCH>((const XT*)a.gate + g * a.ldg, n, tid, vec, gt);
       gate_at = g;
     }
-    float v[NCH][8], mean_post = 0.f, r_post = 1.f, mean_pre, r_pre;
+    float v[NCH][8], hv[NCH][8], mean_post = 0.f, r_post = 1.f, mean_pre, r_pre;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) hv[c][e] = a.residual_scale * (float)hr[c].v[e];
     if (a.y) {
 #pragma unroll
       for (int c = 0; c < NCH; ++c)
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[c][e] = (float)yr[c].v[e];
+    }
+    if (t + stride < a.T) request(t + stride);
+    if (a.y) {
       norm(v, a.post, a.post_eps, a.post_weight, ow, a.post_bias, ob, mean_post, r_post);
 #pragma unroll
       for (int c = 0; c < NCH; ++c)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           if (a.gate) v[c][e] *= (float)gt[c].v[e];
-          v[c][e] += a.residual_scale * (float)hr[c].v[e];
+          v[c][e] += hv[c][e];
         }
     } else {
 #pragma unroll
       for (int c = 0; c < NCH; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[c][e] = a.residual_scale * (float)hr[c].v[e];
+        for (int e = 0; e < 8; ++e) v[c][e] = hv[c][e];
     }
     if (a.h_out) store_row<HT, TPR, NCH>((HT*)a.h_out + t * a.ldho, n, tid, vec, v);
     if (!a.x && !a.q && !a.stats) continue;
@@ -143,18 +156,21 @@ quantize_long_kernel(const XT* __restrict__ X, int64_t T, int64_t n, int64_t ldx
 
 template <typename HT, typename XT, int TPR, int NCH>
 static int launch_norm_cfg(const vnm_residual_norm_args& a, int64_t scale_rows, bool vec, hipStream_t st) {
-  constexpr int RPB = TPR < 256 ? 256 / TPR : 1, THREADS = TPR < 256 ? 256 : TPR;
+  constexpr int RPB = TPR == 64 ? 4 : 1, THREADS = TPR == 64 ? 256 : TPR;
   int64_t blocks = (a.T + RPB - 1) / RPB;
-  if (blocks > 256 * 8) blocks = 256 * 8;
+  const int64_t most = 256 * (16 * 64 / THREADS);         // 16 waves per compute unit, as many as their registers allow
+  if (blocks > most) blocks = most;
   hipLaunchKernelGGL((residual_norm_kernel<HT, XT, TPR, NCH>), dim3((unsigned)blocks), dim3(THREADS), 0, st, a, scale_rows, (int)vec);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) { set_hip_error(e, "residual_norm_kernel"); return VNM_ERR_HIP; }
   return VNM_OK;
 }
+// An octet per thread where a row has at most 8192 channels: with the next row requested ahead a thread needs about 100 registers
+// for each, and fewer waves per SIMD cost more than the barriers of rows that are spread over several.
 template <typename HT, typename XT>
 static int launch_norm(const vnm_residual_norm_args& a, int64_t scale_rows, bool vec, hipStream_t st) {
   if (a.n <= 512) return launch_norm_cfg<HT, XT, 64, 1>(a, scale_rows, vec, st);
-  if (a.n <= 1024) return launch_norm_cfg<HT, XT, 64, 2>(a, scale_rows, vec, st);
+  if (a.n <= 1024) return launch_norm_cfg<HT, XT, 128, 1>(a, scale_rows, vec, st);
   if (a.n <= 2048) return launch_norm_cfg<HT, XT, 256, 1>(a, scale_rows, vec, st);
   if (a.n <= 4096) return launch_norm_cfg<HT, XT, 512, 1>(a, scale_rows, vec, st);
   if (a.n <= 8192) return launch_norm_cfg<HT, XT, 1024, 1>(a, scale_rows, vec, st);

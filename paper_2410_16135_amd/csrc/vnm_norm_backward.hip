@@ -18,8 +18,11 @@ static Cut make_cut(int64_t T, int64_t n, int64_t gate_tokens) {
   Cut c;
   c.tokens = gate_tokens > 0 && gate_tokens < T ? gate_tokens : T > 0 ? T : 1;
   c.groups = T > 0 ? (T + c.tokens - 1) / c.tokens : 0;
-  const int64_t workers = n <= 1024 ? 2048 : 512;
+  // Few tokens: up to 256 workers.  Many: as many as keep the chip busy with a row ahead requested (one wave each up to 1024
+  // channels, a workgroup above), as every worker leaves a row of partial sums to be written and read.
+  const int64_t workers = T <= 1024 ? 256 : n <= 1024 ? 1024 : 512;
   c.per = (T + workers - 1) / workers;
+  if (T > 1024 && c.per < 4) c.per = 4;
   if (c.per < 1) c.per = 1;
   if (c.per > c.tokens) c.per = c.tokens;
   c.pieces = (c.tokens + c.per - 1) / c.per;
@@ -35,9 +38,9 @@ struct BackArgs {
 };
 
 template <typename HT, typename XT, int TPR, int NCH>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
+__global__ void __launch_bounds__(TPR == 64 ? 256 : TPR)
 residual_norm_backward_kernel(const BackArgs b) {
-  constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
+  constexpr int RPB = TPR == 64 ? 4 : 1;
   __shared__ float2 lds[TPR == 64 ? 1 : 2 * (TPR / 64)];
   int turn = 0;
   const vnm_residual_norm_backward_args& a = b.a;
@@ -64,17 +67,27 @@ residual_norm_backward_kernel(const BackArgs b) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[k][c][e] = 0.f;
   const bool through_pre = a.dx && a.pre != VNM_NORM_NONE;
-  for (int64_t t = first; t < end; ++t) {
-    Octet<XT> xr[NCH], yr[NCH];
-    Octet<HT> hr[NCH], gr[NCH];
+  Octet<XT> xr[NCH], yr[NCH];
+  Octet<HT> hr[NCH], gr[NCH];
+  auto request = [&](int64_t t) {
     if (a.dx) load_row<XT, TPR, NCH>((const XT*)a.dx + t * a.lddx, n, tid, vec, xr);
     if (through_pre) load_row<HT, TPR, NCH>((const HT*)a.h_new + t * a.ldh, n, tid, vec, hr);
     if (a.dh_out) load_row<HT, TPR, NCH>((const HT*)a.dh_out + t * a.lddho, n, tid, vec, gr);
     if (a.y) load_row<XT, TPR, NCH>((const XT*)a.y + t * a.ldy, n, tid, vec, yr);
+  };
+  if (first < end) request(first);                       // (the last group may have fewer tokens than pieces)
+  for (int64_t t = first; t < end; ++t) {
     float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
     if (a.stats) st = ((const float4*)a.stats)[t];
-    // d = gradient of h'
-    float d[NCH][8];
+    // d = gradient of h'; the next row is requested when this one's has been taken over into fp32
+    float d[NCH][8], yv[NCH][8], gv[NCH][8];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        yv[c][e] = a.y ? (float)yr[c].v[e] : 0.f;
+        gv[c][e] = a.dh_out ? (float)gr[c].v[e] : 0.f;
+      }
     if (through_pre) {
       float xhat[NCH][8], s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -89,6 +102,7 @@ residual_norm_backward_kernel(const BackArgs b) {
           s1 += d[c][e] * xhat[c][e];                    // (dx is 0 outside the row)
           s2 += d[c][e];
         }
+      if (t + 1 < end) request(t + 1);
       const float2 s = row_sum2<TPR>(s1, s2, lds, turn);
       const float m1 = s.x * inv_n, m2 = a.pre == VNM_NORM_LAYER ? s.y * inv_n : 0.f;
 #pragma unroll
@@ -100,12 +114,13 @@ residual_norm_backward_kernel(const BackArgs b) {
       for (int c = 0; c < NCH; ++c)
 #pragma unroll
         for (int e = 0; e < 8; ++e) d[c][e] = a.dx ? (float)xr[c].v[e] : 0.f;
+      if (t + 1 < end) request(t + 1);
     }
     if (a.dh_out) {
 #pragma unroll
       for (int c = 0; c < NCH; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[c][e] += (float)gr[c].v[e];
+        for (int e = 0; e < 8; ++e) d[c][e] += gv[c][e];
     }
     if (a.dh) {
       float o[NCH][8];
@@ -122,7 +137,7 @@ residual_norm_backward_kernel(const BackArgs b) {
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        yhat[c][e] = a.y ? ((float)yr[c].v[e] - st.x) * st.y : 0.f;
+        yhat[c][e] = a.y ? (yv[c][e] - st.x) * st.y : 0.f;
         const bool inside = (c * TPR + tid) * 8 + e < n;
         if (!inside) d[c][e] = yhat[c][e] = 0.f;         // (the means were taken away outside the row too)
         if (a.d_gate) {
@@ -172,10 +187,11 @@ residual_norm_backward_kernel(const BackArgs b) {
   }
 }
 
-// out[row][i] = sum over the `count` rows of part from row * count on: 32 columns per workgroup, 8 threads per column
+// out[row][i] = sum over the `count` rows of part from row * count on: 32 columns per workgroup, 32 threads per column that
+// request four rows at a time
 struct ReduceArgs { const float* part[kSums]; float* out[kSums]; int64_t rows[kSums], count[kSums]; int64_t n; };
-__global__ void __launch_bounds__(256) column_reduce_kernel(const ReduceArgs r) {
-  __shared__ float lds[8][33];
+__global__ void __launch_bounds__(1024) column_reduce_kernel(const ReduceArgs r) {
+  __shared__ float lds[32][33];
   const int col = threadIdx.x & 31, slice = threadIdx.x >> 5;
   const int64_t i = (int64_t)blockIdx.x * 32 + col;
   const int k = blockIdx.z;
@@ -184,12 +200,17 @@ __global__ void __launch_bounds__(256) column_reduce_kernel(const ReduceArgs r) 
     const float* p = r.part[k] + row * count * r.n;
     float s = 0.f;
     if (i < r.n)
-      for (int64_t w = slice; w < count; w += 8) s += p[w * r.n + i];
+      for (int64_t w = slice; w < count; w += 128) {
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = w + 32 * q < count ? p[(w + 32 * q) * r.n + i] : 0.f;
+        s += (v[0] + v[1]) + (v[2] + v[3]);
+      }
     lds[slice][col] = s;
     __syncthreads();
     if (slice == 0 && i < r.n) {
 #pragma unroll
-      for (int q = 1; q < 8; ++q) s += lds[q][col];
+      for (int q = 1; q < 32; ++q) s += lds[q][col];
       r.out[k][row * r.n + i] = s;
     }
     __syncthreads();
@@ -198,7 +219,7 @@ __global__ void __launch_bounds__(256) column_reduce_kernel(const ReduceArgs r) 
 
 template <typename HT, typename XT, int TPR, int NCH>
 static int launch_back_cfg(const BackArgs& b, hipStream_t st) {
-  constexpr int RPB = TPR < 256 ? 256 / TPR : 1, THREADS = TPR < 256 ? 256 : TPR;
+  constexpr int RPB = TPR == 64 ? 4 : 1, THREADS = TPR == 64 ? 256 : TPR;
   const int64_t blocks = (b.cut.groups * b.cut.pieces + RPB - 1) / RPB;
   if (blocks > 0x7FFFFFFF) return VNM_ERR_UNSUPPORTED;
   hipLaunchKernelGGL((residual_norm_backward_kernel<HT, XT, TPR, NCH>), dim3((unsigned)blocks), dim3(THREADS), 0, st, b);
@@ -209,10 +230,10 @@ static int launch_back_cfg(const BackArgs& b, hipStream_t st) {
 template <typename HT, typename XT>
 static int launch_back(const BackArgs& b, hipStream_t st) {
   if (b.a.n <= 512) return launch_back_cfg<HT, XT, 64, 1>(b, st);
-  if (b.a.n <= 1024) return launch_back_cfg<HT, XT, 64, 2>(b, st);
+  if (b.a.n <= 1024) return launch_back_cfg<HT, XT, 128, 1>(b, st);
   if (b.a.n <= 2048) return launch_back_cfg<HT, XT, 256, 1>(b, st);
   if (b.a.n <= 4096) return launch_back_cfg<HT, XT, 512, 1>(b, st);
-  if (b.a.n <= 8192) return launch_back_cfg<HT, XT, 512, 2>(b, st);
+  if (b.a.n <= 8192) return launch_back_cfg<HT, XT, 1024, 1>(b, st);
   return launch_back_cfg<HT, XT, 1024, 2>(b, st);
 }
 
@@ -304,7 +325,7 @@ extern "C" int vnm_residual_norm_backward(const vnm_residual_norm_backward_args*
   if (!asked) return VNM_OK;
   const int64_t rows = gate_rows(a.T, a.gate_tokens);
   const unsigned gy = (unsigned)(a.d_gate && rows > 1 ? (rows < 65535 ? rows : 65535) : 1);
-  hipLaunchKernelGGL(column_reduce_kernel, dim3((unsigned)((a.n + 31) / 32), gy, (unsigned)asked), dim3(256), 0, st, r);
+  hipLaunchKernelGGL(column_reduce_kernel, dim3((unsigned)((a.n + 31) / 32), gy, (unsigned)asked), dim3(1024), 0, st, r);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) { set_hip_error(e, "column_reduce_kernel"); return VNM_ERR_HIP; }
   return VNM_OK;
