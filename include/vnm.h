@@ -477,8 +477,8 @@ int vnm_residual_norm(const vnm_residual_norm_args* a, void* stream);
  * Each output may be NULL: dh (type h_dtype; gradient of h), dy (type x_dtype), and fp32 sums over the tokens:
  *   d_post_weight, d_post_bias, d_pre_weight, d_pre_bias [n], and d_gate [rows of gate x n], densely stored.
  * dh may be dh_out itself (same leading dimension).  The normalised values are recomputed from h_new and y
- * as they are stored; sums over the tokens are taken in fp32 in an order that depends on T, n and
- * gate_tokens only, so the results are reproducible.
+ * as they are stored; sums over the tokens are taken in fp32 in an order that depends on T, n, gate_tokens
+ * and which arguments are given only, so the results are reproducible.
  *   workspace  dev, 16-byte aligned, vnm_residual_norm_backward_workspace_bytes bytes; contents are scratch
  * T == 0: the sums are set to zero (d_gate, of no rows unless gate_tokens is 0, likewise).
  */

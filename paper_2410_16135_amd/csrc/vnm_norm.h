@@ -7,6 +7,19 @@ namespace vnm {
 // 8 consecutive elements as they are stored: one 16-byte load for 16-bit types, two for fp32
 template <typename T> struct alignas(16) Octet { T v[8]; };
 
+// Says that the octets may change here: values that stay the same from row to row are then widened where they are used and
+// occupy half of the registers between.
+template <typename T, int NCH>
+__device__ __forceinline__ void keep_stored(Octet<T> (&r)[NCH]) {
+  typedef unsigned words __attribute__((ext_vector_type(sizeof(T) * 2)));
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) {
+    words w = __builtin_bit_cast(words, r[c]);
+    asm volatile("" : "+v"(w));
+    r[c] = __builtin_bit_cast(Octet<T>, w);
+  }
+}
+
 // The share of a row that a thread of TPR holds: octets tid, tid + TPR, ...  VEC: rows are 16-byte aligned and n % 8 == 0, so
 // that an octet is inside the row or outside as a whole; otherwise its elements are fetched and stored one by one.
 template <typename T, int TPR, int NCH>
@@ -27,6 +40,25 @@ __device__ __forceinline__ void load_row(const T* p, int n, int tid, bool vec, O
         r[c].v[e] = at < n ? p[at] : (T)0.f;
       }
   }
+}
+// A row of parameters, or of `other` where there is none (the elements past n do not matter)
+template <typename T, int TPR, int NCH>
+__device__ __forceinline__ void load_parameters(const void* p, float other, int n, int tid, bool vec, Octet<T> (&r)[NCH]) {
+  if (p) { load_row<T, TPR, NCH>((const T*)p, n, tid, vec, r); return; }
+#pragma unroll
+  for (int c = 0; c < NCH; ++c)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[c].v[e] = (T)other;
+}
+// Zeros for the elements past n: a branch that all but the last of the row's waves skip
+template <int TPR, int NCH>
+__device__ __forceinline__ void clear_past(float (&x)[NCH][8], int n, int tid) {
+#pragma unroll
+  for (int c = 0; c < NCH; ++c)
+    if ((c * TPR + tid) * 8 + 8 > n) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[c][e] = (c * TPR + tid) * 8 + e < n ? x[c][e] : 0.f;
+    }
 }
 template <typename T, int TPR, int NCH>
 __device__ __forceinline__ void store_row(T* p, int n, int tid, bool vec, const float (&x)[NCH][8]) {

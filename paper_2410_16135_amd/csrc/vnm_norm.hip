@@ -17,18 +17,20 @@ residual_norm_kernel(const vnm_residual_norm_args a, const int64_t scale_rows, c
   int turn = 0;
   const int tid = TPR == 64 ? (threadIdx.x & 63) : threadIdx.x;
   const int n = (int)a.n;
-  const float inv_n = 1.f / (float)n;
-  auto inside = [&](int c, int e) { return (c * TPR + tid) * 8 + e < n; };
+  const float fn = (float)n;
   Octet<XT> ow[NCH], ob[NCH], pw[NCH], pb[NCH], gt[NCH];
-  if (a.post_weight) load_row<XT, TPR, NCH>((const XT*)a.post_weight, n, tid, vec, ow);
-  if (a.post_bias) load_row<XT, TPR, NCH>((const XT*)a.post_bias, n, tid, vec, ob);
-  if (a.pre_weight) load_row<XT, TPR, NCH>((const XT*)a.pre_weight, n, tid, vec, pw);
-  if (a.pre_bias) load_row<XT, TPR, NCH>((const XT*)a.pre_bias, n, tid, vec, pb);
+  if (a.post != VNM_NORM_NONE) {
+    load_parameters<XT, TPR, NCH>(a.post_weight, 1.f, n, tid, vec, ow);
+    load_parameters<XT, TPR, NCH>(a.post_bias, 0.f, n, tid, vec, ob);
+  }
+  if (a.pre != VNM_NORM_NONE) {
+    load_parameters<XT, TPR, NCH>(a.pre_weight, 1.f, n, tid, vec, pw);
+    load_parameters<XT, TPR, NCH>(a.pre_bias, 0.f, n, tid, vec, pb);
+  }
   int64_t gate_at = -1;
 
-  // mean and reciprocal deviation of the row in v, and v normalised
-  auto norm = [&](float (&v)[NCH][8], int kind, float eps, const bool has_w, const Octet<XT> (&w)[NCH], const bool has_b,
-                  const Octet<XT> (&b)[NCH], float& mean, float& r) {
+  // mean and reciprocal deviation of the row in v (zeros past its end, before and after), and v normalised
+  auto norm = [&](float (&v)[NCH][8], int kind, float eps, const Octet<XT> (&w)[NCH], const Octet<XT> (&b)[NCH], float& mean, float& r) {
     mean = 0.f; r = 1.f;
     if (kind == VNM_NORM_NONE) return;
     if (kind == VNM_NORM_LAYER) {
@@ -36,26 +38,25 @@ residual_norm_kernel(const vnm_residual_norm_args a, const int64_t scale_rows, c
 #pragma unroll
       for (int c = 0; c < NCH; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s += v[c][e];        // (0 outside the row)
-      mean = row_sum2<TPR>(s, 0.f, lds, turn).x * inv_n;
+        for (int e = 0; e < 8; ++e) s += v[c][e];
+      mean = row_sum2<TPR>(s, 0.f, lds, turn).x / fn;
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[c][e] -= mean;
+      clear_past<TPR, NCH>(v, n, tid);
     }
     float q = 0.f;
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[c][e] = inside(c, e) ? v[c][e] - mean : 0.f;
-        q += v[c][e] * v[c][e];
-      }
-    r = 1.f / sqrtf(row_sum2<TPR>(q, 0.f, lds, turn).x * inv_n + eps);
+      for (int e = 0; e < 8; ++e) q += v[c][e] * v[c][e];
+    r = 1.f / sqrtf(row_sum2<TPR>(q, 0.f, lds, turn).x / fn + eps);
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[c][e] *= r;
-        if (has_w) v[c][e] *= (float)w[c].v[e];
-        if (has_b) v[c][e] += (float)b[c].v[e];
-      }
+      for (int e = 0; e < 8; ++e) v[c][e] = v[c][e] * r * (float)w[c].v[e] + (float)b[c].v[e];
+    clear_past<TPR, NCH>(v, n, tid);
   };
 
   // The next row is requested when this one's has been taken over into fp32: its way from memory overlaps the reductions.
@@ -74,6 +75,7 @@ residual_norm_kernel(const vnm_residual_norm_args a, const int64_t scale_rows, c
       if (g != gate_at) load_row<XT, TPR, NCH>((const XT*)a.gate + g * a.ldg, n, tid, vec, gt);
       gate_at = g;
     }
+    keep_stored(pw); keep_stored(pb); keep_stored(ow); keep_stored(ob); keep_stored(gt);
     float v[NCH][8], hv[NCH][8], mean_post = 0.f, r_post = 1.f, mean_pre, r_pre;
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
@@ -87,14 +89,18 @@ residual_norm_kernel(const vnm_residual_norm_args a, const int64_t scale_rows, c
     }
     if (t + stride < a.T) request(t + stride);
     if (a.y) {
-      norm(v, a.post, a.post_eps, a.post_weight, ow, a.post_bias, ob, mean_post, r_post);
+      norm(v, a.post, a.post_eps, ow, ob, mean_post, r_post);
+      if (a.gate) {
 #pragma unroll
-      for (int c = 0; c < NCH; ++c)
+        for (int c = 0; c < NCH; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (a.gate) v[c][e] *= (float)gt[c].v[e];
-          v[c][e] += hv[c][e];
-        }
+          for (int e = 0; e < 8; ++e) v[c][e] = v[c][e] * (float)gt[c].v[e] + hv[c][e];
+      } else {
+#pragma unroll
+        for (int c = 0; c < NCH; ++c)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[c][e] += hv[c][e];
+      }
     } else {
 #pragma unroll
       for (int c = 0; c < NCH; ++c)
@@ -103,7 +109,7 @@ residual_norm_kernel(const vnm_residual_norm_args a, const int64_t scale_rows, c
     }
     if (a.h_out) store_row<HT, TPR, NCH>((HT*)a.h_out + t * a.ldho, n, tid, vec, v);
     if (!a.x && !a.q && !a.stats) continue;
-    norm(v, a.pre, a.pre_eps, a.pre_weight, pw, a.pre_bias, pb, mean_pre, r_pre);
+    norm(v, a.pre, a.pre_eps, pw, pb, mean_pre, r_pre);
     if (a.stats && tid == 0) ((float4*)a.stats)[t] = make_float4(mean_post, r_post, mean_pre, r_pre);
     if (a.x) store_row<XT, TPR, NCH>((XT*)a.x + t * a.ldx, n, tid, vec, v);
     if (a.q) {
@@ -112,7 +118,7 @@ residual_norm_kernel(const vnm_residual_norm_args a, const int64_t scale_rows, c
       for (int c = 0; c < NCH; ++c)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const unsigned m = inside(c, e) ? magnitude_bits(v[c][e]) : 0u;
+          const unsigned m = magnitude_bits(v[c][e]);
           top = m > top ? m : top;
         }
       float factor, scale;

@@ -14,13 +14,22 @@ enum { kPreWeight, kPreBias, kPostWeight, kPostBias, kGate, kSums };
 // How the tokens are cut: `groups` gate rows (1 without) of `tokens` tokens each, `pieces` runs of `per` tokens per group.
 struct Cut { int64_t groups, tokens, pieces, per; };
 
-static Cut make_cut(int64_t T, int64_t n, int64_t gate_tokens) {
+// What the call has, kBiases | kGated | kPosted; a kernel for fewer keeps fewer sums and fits more waves.
+enum { kBiases = 1, kGated = 2, kPosted = 4, kAllParts = 7 };
+// Waves per SIMD that the registers are held down for: four where that needs no scratch memory (4096 x 4096 bf16 without a post
+// norm 80 us with three, 45 with four), else three (a gate and biases at 1576 x 384: 20.7 us with four and scratch, 16.3).
+constexpr int back_waves(int TPR, int NCH, int PARTS) {
+  return TPR == 1024 ? 4 : NCH > 1 || PARTS == kAllParts ? 2 : (PARTS & kGated) || (TPR == 64 && PARTS) ? 3 : 4;
+}
+
+static Cut make_cut(int64_t T, int64_t n, int64_t gate_tokens, bool four_waves) {
   Cut c;
   c.tokens = gate_tokens > 0 && gate_tokens < T ? gate_tokens : T > 0 ? T : 1;
   c.groups = T > 0 ? (T + c.tokens - 1) / c.tokens : 0;
-  // Few tokens: up to 256 workers.  Many: as many as keep the chip busy with a row ahead requested (one wave each up to 1024
-  // channels, a workgroup above), as every worker leaves a row of partial sums to be written and read.
-  const int64_t workers = T <= 1024 ? 256 : n <= 1024 ? 1024 : 512;
+  // Few tokens: up to 256 workers.  Many: as many as run at once with four or three waves per SIMD (one more than that and the
+  // call takes two rounds: 12608 x 768 with a gate 61 us in 1802 workers), as every one leaves a row of partial sums.
+  const int64_t per_cu = n <= 512 ? 8 : n <= 1024 ? (four_waves ? 8 : 6) : n <= 2048 ? (four_waves ? 4 : 3) : n <= 4096 ? (four_waves ? 2 : 1) : 1;
+  const int64_t workers = T <= 1024 ? 256 : 256 * per_cu;
   c.per = (T + workers - 1) / workers;
   if (T > 1024 && c.per < 4) c.per = 4;
   if (c.per < 1) c.per = 1;
@@ -37,9 +46,10 @@ struct BackArgs {
   int vec;
 };
 
-template <typename HT, typename XT, int TPR, int NCH>
-__global__ void __launch_bounds__(TPR == 64 ? 256 : TPR)
+template <typename HT, typename XT, int TPR, int NCH, int PARTS>
+__global__ void __launch_bounds__(TPR == 64 ? 256 : TPR, back_waves(TPR, NCH, PARTS))
 residual_norm_backward_kernel(const BackArgs b) {
+  constexpr bool BIASES = PARTS & kBiases, GATED = PARTS & kGated, POSTED = PARTS & kPosted;
   constexpr int RPB = TPR == 64 ? 4 : 1;
   __shared__ float2 lds[TPR == 64 ? 1 : 2 * (TPR / 64)];
   int turn = 0;
@@ -52,13 +62,13 @@ residual_norm_backward_kernel(const BackArgs b) {
   const int64_t group_end = (group + 1) * b.cut.tokens < a.T ? (group + 1) * b.cut.tokens : a.T;
   end = end < group_end ? end : group_end;
   const int n = (int)a.n;
-  const float inv_n = 1.f / (float)n;
+  const float fn = (float)n;
   const bool vec = b.vec;
   Octet<XT> pw[NCH], ow[NCH], ob[NCH], gt[NCH];
-  if (a.pre_weight) load_row<XT, TPR, NCH>((const XT*)a.pre_weight, n, tid, vec, pw);
-  if (a.post_weight) load_row<XT, TPR, NCH>((const XT*)a.post_weight, n, tid, vec, ow);
-  if (a.post_bias) load_row<XT, TPR, NCH>((const XT*)a.post_bias, n, tid, vec, ob);
-  if (a.gate) load_row<XT, TPR, NCH>((const XT*)a.gate + group * a.ldg, n, tid, vec, gt);
+  load_parameters<XT, TPR, NCH>(a.pre_weight, 1.f, n, tid, vec, pw);
+  if (POSTED) load_parameters<XT, TPR, NCH>(a.post_weight, 1.f, n, tid, vec, ow);
+  if (BIASES) load_parameters<XT, TPR, NCH>(a.post_bias, 0.f, n, tid, vec, ob);
+  if (GATED) load_parameters<XT, TPR, NCH>(a.gate ? (const XT*)a.gate + group * a.ldg : nullptr, 1.f, n, tid, vec, gt);
   float sum[kSums][NCH][8];
 #pragma unroll
   for (int k = 0; k < kSums; ++k)
@@ -67,9 +77,13 @@ residual_norm_backward_kernel(const BackArgs b) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[k][c][e] = 0.f;
   const bool through_pre = a.dx && a.pre != VNM_NORM_NONE;
-  Octet<XT> xr[NCH], yr[NCH];
+  Octet<XT> xr[NCH], yr[NCH];                            // (zeros for a gradient or an output that is not there)
   Octet<HT> hr[NCH], gr[NCH];
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) { xr[c] = yr[c] = Octet<XT>{}; hr[c] = gr[c] = Octet<HT>{}; }
+  float4 next_stats = make_float4(0.f, 1.f, 0.f, 1.f);
   auto request = [&](int64_t t) {
+    if (a.stats) next_stats = ((const float4*)a.stats)[t];
     if (a.dx) load_row<XT, TPR, NCH>((const XT*)a.dx + t * a.lddx, n, tid, vec, xr);
     if (through_pre) load_row<HT, TPR, NCH>((const HT*)a.h_new + t * a.ldh, n, tid, vec, hr);
     if (a.dh_out) load_row<HT, TPR, NCH>((const HT*)a.dh_out + t * a.lddho, n, tid, vec, gr);
@@ -77,16 +91,16 @@ residual_norm_backward_kernel(const BackArgs b) {
   };
   if (first < end) request(first);                       // (the last group may have fewer tokens than pieces)
   for (int64_t t = first; t < end; ++t) {
-    float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
-    if (a.stats) st = ((const float4*)a.stats)[t];
+    const float4 st = next_stats;
+    keep_stored(pw); keep_stored(ow); keep_stored(ob); keep_stored(gt);
     // d = gradient of h'; the next row is requested when this one's has been taken over into fp32
     float d[NCH][8], yv[NCH][8], gv[NCH][8];
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        yv[c][e] = a.y ? (float)yr[c].v[e] : 0.f;
-        gv[c][e] = a.dh_out ? (float)gr[c].v[e] : 0.f;
+        yv[c][e] = (float)yr[c].v[e];
+        gv[c][e] = (float)gr[c].v[e];
       }
     if (through_pre) {
       float xhat[NCH][8], s1 = 0.f, s2 = 0.f;
@@ -97,14 +111,14 @@ residual_norm_backward_kernel(const BackArgs b) {
           const float dx = (float)xr[c].v[e];
           xhat[c][e] = ((float)hr[c].v[e] - st.z) * st.w;
           sum[kPreWeight][c][e] += dx * xhat[c][e];
-          sum[kPreBias][c][e] += dx;
-          d[c][e] = a.pre_weight ? dx * (float)pw[c].v[e] : dx;
+          if (BIASES) sum[kPreBias][c][e] += dx;
+          d[c][e] = dx * (float)pw[c].v[e];
           s1 += d[c][e] * xhat[c][e];                    // (dx is 0 outside the row)
           s2 += d[c][e];
         }
       if (t + 1 < end) request(t + 1);
       const float2 s = row_sum2<TPR>(s1, s2, lds, turn);
-      const float m1 = s.x * inv_n, m2 = a.pre == VNM_NORM_LAYER ? s.y * inv_n : 0.f;
+      const float m1 = s.x / fn, m2 = a.pre == VNM_NORM_LAYER ? s.y / fn : 0.f;
 #pragma unroll
       for (int c = 0; c < NCH; ++c)
 #pragma unroll
@@ -113,15 +127,13 @@ residual_norm_backward_kernel(const BackArgs b) {
 #pragma unroll
       for (int c = 0; c < NCH; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[c][e] = a.dx ? (float)xr[c].v[e] : 0.f;
+        for (int e = 0; e < 8; ++e) d[c][e] = (float)xr[c].v[e];
       if (t + 1 < end) request(t + 1);
     }
-    if (a.dh_out) {
 #pragma unroll
-      for (int c = 0; c < NCH; ++c)
+    for (int c = 0; c < NCH; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[c][e] += gv[c][e];
-    }
+      for (int e = 0; e < 8; ++e) d[c][e] += gv[c][e];
     if (a.dh) {
       float o[NCH][8];
 #pragma unroll
@@ -136,29 +148,32 @@ residual_norm_backward_kernel(const BackArgs b) {
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
+      for (int e = 0; e < 8; ++e) yhat[c][e] = (yv[c][e] - st.x) * st.y;
+    clear_past<TPR, NCH>(yhat, n, tid);
+    clear_past<TPR, NCH>(d, n, tid);                     // (means were taken away past the row's end too)
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
       for (int e = 0; e < 8; ++e) {
-        yhat[c][e] = a.y ? (yv[c][e] - st.x) * st.y : 0.f;
-        const bool inside = (c * TPR + tid) * 8 + e < n;
-        if (!inside) d[c][e] = yhat[c][e] = 0.f;         // (the means were taken away outside the row too)
-        if (a.d_gate) {
+        if (GATED) {
           float p = yhat[c][e];
-          if (a.post_weight) p *= (float)ow[c].v[e];
-          if (a.post_bias) p += (float)ob[c].v[e];
+          if (POSTED) p *= (float)ow[c].v[e];
+          if (BIASES) p += (float)ob[c].v[e];
           sum[kGate][c][e] += d[c][e] * p;
+          d[c][e] *= (float)gt[c].v[e];
         }
-        if (a.gate) d[c][e] *= (float)gt[c].v[e];
-        if (a.post != VNM_NORM_NONE) {
+        if (POSTED) {
           sum[kPostWeight][c][e] += d[c][e] * yhat[c][e];
-          sum[kPostBias][c][e] += d[c][e];
-          if (a.post_weight) d[c][e] *= (float)ow[c].v[e];
+          if (BIASES) sum[kPostBias][c][e] += d[c][e];
+          d[c][e] *= (float)ow[c].v[e];
           s1 += d[c][e] * yhat[c][e];
           s2 += d[c][e];
         }
       }
     if (!a.dy) continue;
-    if (a.post != VNM_NORM_NONE) {
+    if (POSTED && a.post != VNM_NORM_NONE) {               // (rows past 8192 channels have the kernel of all parts)
       const float2 s = row_sum2<TPR>(s1, s2, lds, turn);
-      const float m1 = s.x * inv_n, m2 = a.post == VNM_NORM_LAYER ? s.y * inv_n : 0.f;
+      const float m1 = s.x / fn, m2 = a.post == VNM_NORM_LAYER ? s.y / fn : 0.f;
 #pragma unroll
       for (int c = 0; c < NCH; ++c)
 #pragma unroll
@@ -169,7 +184,7 @@ residual_norm_backward_kernel(const BackArgs b) {
   // the worker's row of every sum that is asked for
 #pragma unroll
   for (int k = 0; k < kSums; ++k) {
-    if (b.part_at[k] < 0) continue;
+    if (b.part_at[k] < 0) continue;                      // (the parts that the kernel lacks are not asked for)
     float* p = b.part + b.part_at[k] + worker * n;
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
@@ -187,54 +202,71 @@ residual_norm_backward_kernel(const BackArgs b) {
   }
 }
 
-// out[row][i] = sum over the `count` rows of part from row * count on: 32 columns per workgroup, 32 threads per column that
-// request four rows at a time
+// out[row][i] = sum over the `count` rows of part from row * count on: 16 columns per workgroup, 64 threads per column that
+// request eight rows at a time
 struct ReduceArgs { const float* part[kSums]; float* out[kSums]; int64_t rows[kSums], count[kSums]; int64_t n; };
 __global__ void __launch_bounds__(1024) column_reduce_kernel(const ReduceArgs r) {
-  __shared__ float lds[32][33];
-  const int col = threadIdx.x & 31, slice = threadIdx.x >> 5;
-  const int64_t i = (int64_t)blockIdx.x * 32 + col;
+  __shared__ float lds[64][17];
+  const int col = threadIdx.x & 15, slice = threadIdx.x >> 4;
+  const int64_t i = (int64_t)blockIdx.x * 16 + col;
   const int k = blockIdx.z;
   for (int64_t row = blockIdx.y; row < r.rows[k]; row += gridDim.y) {
     const int64_t count = r.count[k];
     const float* p = r.part[k] + row * count * r.n;
     float s = 0.f;
     if (i < r.n)
-      for (int64_t w = slice; w < count; w += 128) {
-        float v[4];
+      for (int64_t w = slice; w < count; w += 512) {
+        float v[8];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = w + 32 * q < count ? p[(w + 32 * q) * r.n + i] : 0.f;
-        s += (v[0] + v[1]) + (v[2] + v[3]);
+        for (int q = 0; q < 8; ++q) v[q] = w + 64 * q < count ? p[(w + 64 * q) * r.n + i] : 0.f;
+        s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
       }
     lds[slice][col] = s;
     __syncthreads();
-    if (slice == 0 && i < r.n) {
+    if (slice < 4) {
 #pragma unroll
-      for (int q = 1; q < 32; ++q) s += lds[q][col];
-      r.out[k][row * r.n + i] = s;
+      for (int q = 1; q < 16; ++q) s += lds[slice + 4 * q][col];
+      lds[slice][col] = s;                                // (only its own thread has read this entry)
     }
+    __syncthreads();
+    if (slice == 0 && i < r.n) r.out[k][row * r.n + i] = (lds[0][col] + lds[1][col]) + (lds[2][col] + lds[3][col]);
     __syncthreads();
   }
 }
 
-template <typename HT, typename XT, int TPR, int NCH>
+template <typename HT, typename XT, int TPR, int NCH, int PARTS>
 static int launch_back_cfg(const BackArgs& b, hipStream_t st) {
   constexpr int RPB = TPR == 64 ? 4 : 1, THREADS = TPR == 64 ? 256 : TPR;
   const int64_t blocks = (b.cut.groups * b.cut.pieces + RPB - 1) / RPB;
   if (blocks > 0x7FFFFFFF) return VNM_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL((residual_norm_backward_kernel<HT, XT, TPR, NCH>), dim3((unsigned)blocks), dim3(THREADS), 0, st, b);
+  hipLaunchKernelGGL((residual_norm_backward_kernel<HT, XT, TPR, NCH, PARTS>), dim3((unsigned)blocks), dim3(THREADS), 0, st, b);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) { set_hip_error(e, "residual_norm_backward_kernel"); return VNM_ERR_HIP; }
   return VNM_OK;
 }
+template <typename HT, typename XT, int PARTS>
+static int launch_back_parts(const BackArgs& b, hipStream_t st) {
+  if (b.a.n <= 512) return launch_back_cfg<HT, XT, 64, 1, PARTS>(b, st);
+  if (b.a.n <= 1024) return launch_back_cfg<HT, XT, 128, 1, PARTS>(b, st);
+  if (b.a.n <= 2048) return launch_back_cfg<HT, XT, 256, 1, PARTS>(b, st);
+  if (b.a.n <= 4096) return launch_back_cfg<HT, XT, 512, 1, PARTS>(b, st);
+  if (b.a.n <= 8192) return launch_back_cfg<HT, XT, 1024, 1, PARTS>(b, st);
+  return launch_back_cfg<HT, XT, 1024, 2, kAllParts>(b, st);
+}
+static int parts_of(const vnm_residual_norm_backward_args& a) {
+  const bool biases = a.post_bias || a.d_post_bias || a.d_pre_bias, gated = a.gate || a.d_gate;
+  if (a.post != VNM_NORM_NONE) return biases || gated ? kAllParts : kPosted;
+  return gated ? kBiases | kGated : biases ? kBiases : 0;
+}
 template <typename HT, typename XT>
 static int launch_back(const BackArgs& b, hipStream_t st) {
-  if (b.a.n <= 512) return launch_back_cfg<HT, XT, 64, 1>(b, st);
-  if (b.a.n <= 1024) return launch_back_cfg<HT, XT, 128, 1>(b, st);
-  if (b.a.n <= 2048) return launch_back_cfg<HT, XT, 256, 1>(b, st);
-  if (b.a.n <= 4096) return launch_back_cfg<HT, XT, 512, 1>(b, st);
-  if (b.a.n <= 8192) return launch_back_cfg<HT, XT, 1024, 1>(b, st);
-  return launch_back_cfg<HT, XT, 1024, 2>(b, st);
+  switch (parts_of(b.a)) {
+    case kAllParts: return launch_back_parts<HT, XT, kAllParts>(b, st);
+    case kPosted: return launch_back_parts<HT, XT, kPosted>(b, st);
+    case kBiases | kGated: return launch_back_parts<HT, XT, kBiases | kGated>(b, st);
+    case kBiases: return launch_back_parts<HT, XT, kBiases>(b, st);
+  }
+  return launch_back_parts<HT, XT, 0>(b, st);
 }
 
 static int64_t gate_rows(int64_t T, int64_t gate_tokens) { return gate_tokens > 0 ? (T + gate_tokens - 1) / gate_tokens : 1; }
@@ -250,7 +282,7 @@ extern "C" int vnm_residual_norm_backward_workspace_bytes(int64_t T, int64_t n, 
   if (!bytes) return VNM_ERR_NULL;
   if (T < 0 || n <= 0 || gate_tokens < 0) return VNM_ERR_SHAPE;
   if (n > VNM_NORM_MAX_CHANNELS) return VNM_ERR_UNSUPPORTED;
-  const Cut c = make_cut(T, n, gate_tokens);
+  const Cut c = make_cut(T, n, gate_tokens, true);       // (the most workers)
   const int64_t each = (c.groups * c.pieces * n * 4 + 255) / 256 * 256;
   *bytes = kSums * each + 256;
   return VNM_OK;
@@ -291,7 +323,8 @@ extern "C" int vnm_residual_norm_backward(const vnm_residual_norm_backward_args*
   if (a.T != 0 && any_sum && !workspace) return VNM_ERR_WORKSPACE;
   BackArgs b;
   b.a = a;
-  b.cut = make_cut(a.T, a.n, a.gate_tokens);
+  const int parts = parts_of(a);
+  b.cut = make_cut(a.T, a.n, a.gate_tokens, parts != kAllParts && !(parts & kGated));
   const int64_t workers = b.cut.groups * b.cut.pieces, each = (workers * a.n * 4 + 255) / 256 * 256;
   void* const outs[kSums] = {a.d_pre_weight, a.d_pre_bias, a.d_post_weight, a.d_post_bias, a.d_gate};
   ReduceArgs r{};
@@ -325,7 +358,7 @@ extern "C" int vnm_residual_norm_backward(const vnm_residual_norm_backward_args*
   if (!asked) return VNM_OK;
   const int64_t rows = gate_rows(a.T, a.gate_tokens);
   const unsigned gy = (unsigned)(a.d_gate && rows > 1 ? (rows < 65535 ? rows : 65535) : 1);
-  hipLaunchKernelGGL(column_reduce_kernel, dim3((unsigned)((a.n + 31) / 32), gy, (unsigned)asked), dim3(1024), 0, st, r);
+  hipLaunchKernelGGL(column_reduce_kernel, dim3((unsigned)((a.n + 15) / 16), gy, (unsigned)asked), dim3(1024), 0, st, r);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) { set_hip_error(e, "column_reduce_kernel"); return VNM_ERR_HIP; }
   return VNM_OK;
