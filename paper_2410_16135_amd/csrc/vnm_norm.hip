@@ -9,9 +9,25 @@
 
 namespace vnm {
 
+// 8 values of a row as int8
+template <typename F>
+__device__ __forceinline__ void store_i8(unsigned char* q, int n, int at, bool vec, float factor, F value) {
+  unsigned b[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) b[e] = i8_round(value(e), factor);
+  uint2 o = make_uint2(i8_pack4(b[0], b[1], b[2], b[3]), i8_pack4(b[4], b[5], b[6], b[7]));
+  if (!(factor > 0.f)) o = make_uint2(0, 0);               // (no value of such a row counts; an infinity times 0 is none)
+  if (vec) {
+    if (at < n) *(uint2*)(q + at) = o;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) if (at + e < n) q[at + e] = (unsigned char)((e < 4 ? o.x : o.y) >> (8 * (e & 3)));
+  }
+}
+
 template <typename HT, typename XT, int TPR, int NCH>
 __global__ void __launch_bounds__(TPR == 64 ? 256 : TPR)
-residual_norm_kernel(const vnm_residual_norm_args a, const int64_t scale_rows, const int vec) {
+residual_norm_kernel(const vnm_residual_norm_args a, const int vec) {
   constexpr int RPB = TPR == 64 ? 4 : 1;         // rows that a workgroup has at a time
   __shared__ float2 lds[TPR == 64 ? 1 : 2 * (TPR / 64)];
   int turn = 0;
@@ -123,22 +139,46 @@ residual_norm_kernel(const vnm_residual_norm_args a, const int64_t scale_rows, c
         }
       float factor, scale;
       i8_factor(__builtin_bit_cast(float, row_max<TPR>(top, lds, turn)), &factor, &scale);
-      if (tid == 0 && t < scale_rows) ((float*)a.q_scale)[t] = scale;
+      if (tid == 0) ((float*)a.q_scale)[t] = scale;
       unsigned char* q = (unsigned char*)a.q + t * a.ldq;
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) {
-        const int at = (c * TPR + tid) * 8;
-        unsigned b[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) b[e] = factor > 0.f ? i8_round(v[c][e], factor) : 0u;
-        if (vec) {
-          if (at < n) *(uint2*)(q + at) = make_uint2(i8_pack4(b[0], b[1], b[2], b[3]), i8_pack4(b[4], b[5], b[6], b[7]));
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) if (at + e < n) q[at + e] = (unsigned char)b[e];
-        }
-      }
+      for (int c = 0; c < NCH; ++c) store_i8(q, n, (c * TPR + tid) * 8, vec, factor, [&](int e) { return v[c][e]; });
     }
+  }
+}
+
+// vnm_quantize_x: the largest magnitude of a row and then its int8 values, from registers.  Bound by memory (the reductions leave it
+// idle, so the next row is requested before them).
+template <typename XT, int TPR, int NCH>
+__global__ void __launch_bounds__(TPR == 64 ? 256 : TPR)
+quantize_rows_kernel(const XT* __restrict__ X, int64_t T, int n, int64_t ldx, unsigned char* __restrict__ Q, int64_t ldq,
+                     float* __restrict__ scales, int64_t scale_rows, const int vec) {
+  constexpr int RPB = TPR == 64 ? 4 : 1;
+  __shared__ float2 lds[TPR == 64 ? 1 : 2 * (TPR / 64)];
+  int turn = 0;
+  const int tid = TPR == 64 ? (threadIdx.x & 63) : threadIdx.x;
+  const int64_t first = (int64_t)blockIdx.x * RPB + (TPR == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
+  const int64_t stride = (int64_t)gridDim.x * RPB;
+  Octet<XT> next[NCH], x[NCH];
+  if (first < T) load_row<XT, TPR, NCH>(X + first * ldx, n, tid, vec, next);
+  for (int64_t t = first; t < T; t += stride) {
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) x[c] = next[c];
+    if (t + stride < T) load_row<XT, TPR, NCH>(X + (t + stride) * ldx, n, tid, vec, next);
+    unsigned top = 0;                                      // (zeros past the row's end)
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const unsigned m = magnitude_bits((float)x[c].v[e]);
+        top = m > top ? m : top;
+      }
+    float factor, scale;
+    i8_factor(__builtin_bit_cast(float, row_max<TPR>(top, lds, turn)), &factor, &scale);
+    if (tid == 0 && t < scale_rows) scales[t] = scale;
+    unsigned char* q = Q + t * ldq;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) store_i8(q, n, (c * TPR + tid) * 8, vec, factor, [&](int e) { return (float)x[c].v[e]; });
   }
 }
 
@@ -161,12 +201,12 @@ quantize_long_kernel(const XT* __restrict__ X, int64_t T, int64_t n, int64_t ldx
 }
 
 template <typename HT, typename XT, int TPR, int NCH>
-static int launch_norm_cfg(const vnm_residual_norm_args& a, int64_t scale_rows, bool vec, hipStream_t st) {
+static int launch_norm_cfg(const vnm_residual_norm_args& a, bool vec, hipStream_t st) {
   constexpr int RPB = TPR == 64 ? 4 : 1, THREADS = TPR == 64 ? 256 : TPR;
   int64_t blocks = (a.T + RPB - 1) / RPB;
   const int64_t most = 256 * (16 * 64 / THREADS);         // 16 waves per compute unit, as many as their registers allow
   if (blocks > most) blocks = most;
-  hipLaunchKernelGGL((residual_norm_kernel<HT, XT, TPR, NCH>), dim3((unsigned)blocks), dim3(THREADS), 0, st, a, scale_rows, (int)vec);
+  hipLaunchKernelGGL((residual_norm_kernel<HT, XT, TPR, NCH>), dim3((unsigned)blocks), dim3(THREADS), 0, st, a, (int)vec);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) { set_hip_error(e, "residual_norm_kernel"); return VNM_ERR_HIP; }
   return VNM_OK;
@@ -174,19 +214,19 @@ static int launch_norm_cfg(const vnm_residual_norm_args& a, int64_t scale_rows, 
 // An octet per thread where a row has at most 8192 channels: with the next row requested ahead a thread needs about 100 registers
 // for each, and fewer waves per SIMD cost more than the barriers of rows that are spread over several.
 template <typename HT, typename XT>
-static int launch_norm(const vnm_residual_norm_args& a, int64_t scale_rows, bool vec, hipStream_t st) {
-  if (a.n <= 512) return launch_norm_cfg<HT, XT, 64, 1>(a, scale_rows, vec, st);
-  if (a.n <= 1024) return launch_norm_cfg<HT, XT, 128, 1>(a, scale_rows, vec, st);
-  if (a.n <= 2048) return launch_norm_cfg<HT, XT, 256, 1>(a, scale_rows, vec, st);
-  if (a.n <= 4096) return launch_norm_cfg<HT, XT, 512, 1>(a, scale_rows, vec, st);
-  if (a.n <= 8192) return launch_norm_cfg<HT, XT, 1024, 1>(a, scale_rows, vec, st);
-  return launch_norm_cfg<HT, XT, 1024, 2>(a, scale_rows, vec, st);
+static int launch_norm(const vnm_residual_norm_args& a, bool vec, hipStream_t st) {
+  if (a.n <= 512) return launch_norm_cfg<HT, XT, 64, 1>(a, vec, st);
+  if (a.n <= 1024) return launch_norm_cfg<HT, XT, 128, 1>(a, vec, st);
+  if (a.n <= 2048) return launch_norm_cfg<HT, XT, 256, 1>(a, vec, st);
+  if (a.n <= 4096) return launch_norm_cfg<HT, XT, 512, 1>(a, vec, st);
+  if (a.n <= 8192) return launch_norm_cfg<HT, XT, 1024, 1>(a, vec, st);
+  return launch_norm_cfg<HT, XT, 1024, 2>(a, vec, st);
 }
-static int launch_norm_types(const vnm_residual_norm_args& a, int64_t scale_rows, bool vec, hipStream_t st) {
-  if (a.x_dtype == VNM_F32) return launch_norm<float, float>(a, scale_rows, vec, st);
+static int launch_norm_types(const vnm_residual_norm_args& a, bool vec, hipStream_t st) {
+  if (a.x_dtype == VNM_F32) return launch_norm<float, float>(a, vec, st);
   if (a.h_dtype == VNM_F32)
-    return a.x_dtype == VNM_F16 ? launch_norm<float, _Float16>(a, scale_rows, vec, st) : launch_norm<float, __bf16>(a, scale_rows, vec, st);
-  return a.x_dtype == VNM_F16 ? launch_norm<_Float16, _Float16>(a, scale_rows, vec, st) : launch_norm<__bf16, __bf16>(a, scale_rows, vec, st);
+    return a.x_dtype == VNM_F16 ? launch_norm<float, _Float16>(a, vec, st) : launch_norm<float, __bf16>(a, vec, st);
+  return a.x_dtype == VNM_F16 ? launch_norm<_Float16, _Float16>(a, vec, st) : launch_norm<__bf16, __bf16>(a, vec, st);
 }
 
 template <typename XT>
@@ -199,18 +239,37 @@ static int launch_quantize_long(const void* X, int64_t T, int64_t n, int64_t ldx
   return VNM_OK;
 }
 
+template <typename XT, int TPR, int NCH>
+static int launch_quantize_cfg(const void* X, int64_t T, int64_t n, int64_t ldx, void* Q, int64_t ldq, void* scale, int64_t scale_rows,
+                               bool vec, hipStream_t st) {
+  constexpr int RPB = TPR == 64 ? 4 : 1, THREADS = TPR == 64 ? 256 : TPR;
+  int64_t blocks = (T + RPB - 1) / RPB;
+  const int64_t most = 256 * (32 * 64 / THREADS);         // 32 waves per compute unit
+  if (blocks > most) blocks = most;
+  hipLaunchKernelGGL((quantize_rows_kernel<XT, TPR, NCH>), dim3((unsigned)blocks), dim3(THREADS), 0, st, (const XT*)X, T, (int)n, ldx,
+                     (unsigned char*)Q, ldq, (float*)scale, scale_rows, (int)vec);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) { set_hip_error(e, "quantize_rows_kernel"); return VNM_ERR_HIP; }
+  return VNM_OK;
+}
+template <typename XT>
+static int launch_quantize(const void* X, int64_t T, int64_t n, int64_t ldx, void* Q, int64_t ldq, void* scale, int64_t scale_rows, hipStream_t st) {
+  const bool vec = n % 8 == 0 && ldx % 8 == 0 && ldq % 8 == 0 && ((uintptr_t)X & 15) == 0 && ((uintptr_t)Q & 7) == 0;
+  if (n > VNM_NORM_MAX_CHANNELS) return launch_quantize_long<XT>(X, T, n, ldx, Q, ldq, scale, scale_rows, st);
+  if (n <= 512) return launch_quantize_cfg<XT, 64, 1>(X, T, n, ldx, Q, ldq, scale, scale_rows, vec, st);
+  if (n <= 1024) return launch_quantize_cfg<XT, 64, 2>(X, T, n, ldx, Q, ldq, scale, scale_rows, vec, st);
+  if (n <= 2048) return launch_quantize_cfg<XT, 256, 1>(X, T, n, ldx, Q, ldq, scale, scale_rows, vec, st);
+  if (n <= 4096) return launch_quantize_cfg<XT, 256, 2>(X, T, n, ldx, Q, ldq, scale, scale_rows, vec, st);
+  if (n <= 8192) return launch_quantize_cfg<XT, 512, 2>(X, T, n, ldx, Q, ldq, scale, scale_rows, vec, st);
+  return launch_quantize_cfg<XT, 1024, 2>(X, T, n, ldx, Q, ldq, scale, scale_rows, vec, st);
+}
+
 // rows from scale_rows on have no scale to store
 int launch_quantize_rows(const void* X, int64_t T, int64_t n, int64_t ldx, int x_dtype, void* Q, int64_t ldq, void* scale,
                          int64_t scale_rows, hipStream_t st) {
-  if (n > VNM_NORM_MAX_CHANNELS)
-    return x_dtype == VNM_F32   ? launch_quantize_long<float>(X, T, n, ldx, Q, ldq, scale, scale_rows, st)
-           : x_dtype == VNM_F16 ? launch_quantize_long<_Float16>(X, T, n, ldx, Q, ldq, scale, scale_rows, st)
-                                : launch_quantize_long<__bf16>(X, T, n, ldx, Q, ldq, scale, scale_rows, st);
-  vnm_residual_norm_args a{};
-  a.T = T; a.n = n; a.h_dtype = a.x_dtype = x_dtype; a.residual_scale = 1.f;
-  a.h = X; a.ldh = ldx; a.q = Q; a.ldq = ldq; a.q_scale = scale;
-  const bool vec = n % 8 == 0 && ldx % 8 == 0 && ldq % 8 == 0 && ((uintptr_t)X & 15) == 0 && ((uintptr_t)Q & 7) == 0;
-  return launch_norm_types(a, scale_rows, vec, st);
+  return x_dtype == VNM_F32   ? launch_quantize<float>(X, T, n, ldx, Q, ldq, scale, scale_rows, st)
+         : x_dtype == VNM_F16 ? launch_quantize<_Float16>(X, T, n, ldx, Q, ldq, scale, scale_rows, st)
+                              : launch_quantize<__bf16>(X, T, n, ldx, Q, ldq, scale, scale_rows, st);
 }
 
 }  // namespace vnm
@@ -256,5 +315,5 @@ extern "C" int vnm_residual_norm(const vnm_residual_norm_args* args, void* strea
   const int64_t lds = a.ldh | (a.y ? a.ldy : 0) | (a.gate && a.gate_tokens ? a.ldg : 0) | (a.h_out ? a.ldho : 0) | (a.x ? a.ldx : 0) |
                       (a.q ? a.ldq : 0);
   const bool vec = a.n % 8 == 0 && lds % 8 == 0 && ((hp | xp) & 15) == 0 && ((uintptr_t)a.q & 7) == 0;
-  return launch_norm_types(a, a.T, vec, (hipStream_t)stream);
+  return launch_norm_types(a, vec, (hipStream_t)stream);
 }
