@@ -683,19 +683,27 @@ def vnm_quantize_x(X, Q=None, scale=None):
     Q = rint(X * ((1 / max|X_t|) * 127)), scale = max|X_t| * (1 / 127).  A fresh Q has rows 16 bytes aligned."""
     import torch
     assert X.is_cuda and X.dim() == 2
-    T, n = X.shape
     dev = X.device
+    if _current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return vnm_quantize_x(X, Q, scale)
+    T, n = X.shape
     ldx = _rows("X", X, T, n, dev)
     if Q is None:
-        Q, ldq = _empty_i8_rows(T, n, dev), (n + 15) // 16 * 16
+        ldq = (n + 15) // 16 * 16
+        Q = torch.empty((T, ldq), dtype=torch.int8, device=dev)
+        if ldq != n:
+            Q = Q[:, :n]
     else:
         ldq = _rows("Q", Q, T, n, dev, torch.int8)
     if scale is None:
         scale = torch.empty(T, dtype=torch.float32, device=dev)
     else:
         _vector("scale", scale, T, dev, torch.float32)
-    _launch("vnm_quantize_x", load_library().vnm_quantize_x, dev, X.data_ptr(), T, n, ldx, _dtype_code(X.dtype), Q.data_ptr(),
-            ldq, scale.data_ptr())
+    status = (_LIB or load_library()).vnm_quantize_x(X.data_ptr(), T, n, ldx, _dtype_code(X.dtype), Q.data_ptr(), ldq,
+                                                     scale.data_ptr(), _raw_stream(dev))
+    if status:
+        _check(status, "vnm_quantize_x")
     return Q, scale
 
 
@@ -772,25 +780,31 @@ def vnm_spmm_i8(Q, scale, c: CompressedI8, bias=None, N: int = 2, out_dtype=None
     vnm_spmm_i8_workspace_bytes(T, c) bytes; by default the call takes one from torch's allocator."""
     import torch
     assert Q.is_cuda and Q.dim() == 2
-    T, dev = Q.shape[0], Q.device
-    out, inn, values = c.out, c.inn, c.values
+    dev = Q.device
+    if _current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return vnm_spmm_i8(Q, scale, c, bias, N, out_dtype, path, Y, workspace)
+    T, inn = Q.shape
+    out, packed = c.out, c.packed
+    assert inn == c.inn and c.values.device == dev
     ldq = _rows("Q", Q, T, inn, dev, torch.int8)
     if T == 1:
         ldq = (inn + 15) // 16 * 16              # (one row: whatever the view's stride)
-    assert values.device == dev
     if Y is None:
         Y, ldy = torch.empty((T, out), dtype=out_dtype or torch.float16, device=dev), out
     else:
         ldy = _rows("Y", Y, T, out, dev)
-    packed = c.packed
     if workspace is None and packed is not None and path != PATH_GENERIC:
         need = _spmm_i8_workspace_bytes(T, out, inn, c.V, N, c.M)
         if need:
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    _launch("vnm_spmm_i8", load_library().vnm_spmm_i8, dev, Q.data_ptr(), T, ldq, _vector("scale", scale, T, dev, torch.float32),
-            values.data_ptr(), c.meta.data_ptr(), c.colidx.data_ptr(), _ptr(packed), _vector("c.scale", c.scale, out, dev, torch.float32),
-            out, inn, c.V, N, c.M, _vector("bias", bias, out, dev, torch.float16), Y.data_ptr(), ldy, _dtype_code(Y.dtype),
-            path, _ptr(workspace), 0 if workspace is None else workspace.numel())
+    status = (_LIB or load_library()).vnm_spmm_i8(
+        Q.data_ptr(), T, ldq, _vector("scale", scale, T, dev, torch.float32), c.values.data_ptr(), c.meta.data_ptr(),
+        c.colidx.data_ptr(), 0 if packed is None else packed.data_ptr(), c.scale.data_ptr(), out, inn, c.V, N, c.M,
+        _vector("bias", bias, out, dev, torch.float16), Y.data_ptr(), ldy, _dtype_code(Y.dtype), path, _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _raw_stream(dev))
+    if status:
+        _check(status, "vnm_spmm_i8")
     return Y
 
 
@@ -816,13 +830,13 @@ class ResidualNormGrads(NamedTuple):
     pre_bias: object
 
 
-def _norm_operands(h, y, gate, gate_tokens, post, pre, x_dtype, vectors):
+def _norm_operands(h, y, gate, gate_tokens, x_dtype, vectors):
     """Shared checks of the two norm calls: (T, n, device, x type, leading dimensions of h, y and gate)."""
     assert h.is_cuda and h.dim() == 2
     T, n = h.shape
     dev = h.device
     if x_dtype is None:
-        x_dtype = next((t.dtype for t in (y, *vectors) if t is not None), h.dtype)
+        x_dtype = y.dtype if y is not None else next((t.dtype for t in vectors if t is not None), h.dtype)
     ldh = _rows("h", h, T, n, dev)
     ldy = 0 if y is None else _rows("y", y, T, n, dev, x_dtype)
     ldg = 0
@@ -846,8 +860,7 @@ def vnm_residual_norm(h, y=None, gate=None, gate_tokens: int = 0, residual_scale
     which is x's too (`x_dtype` where there is none of them).  int8: x leaves as int8 rows with a scale per token, ready for
     vnm_spmm_i8.  h_out: a tensor for h' (h itself: in place); a fresh one by default."""
     import torch
-    T, n, dev, xt, ldh, ldy, ldg = _norm_operands(h, y, gate, gate_tokens, post, pre, x_dtype,
-                                                  (post_weight, post_bias, pre_weight, pre_bias))
+    T, n, dev, xt, ldh, ldy, ldg = _norm_operands(h, y, gate, gate_tokens, x_dtype, (post_weight, post_bias, pre_weight, pre_bias))
     if h_out is None:
         h_out, ldho = torch.empty((T, n), dtype=h.dtype, device=dev), n
     else:
@@ -876,7 +889,7 @@ def vnm_residual_norm_backward(h, stats, dx=None, dh=None, y=None, gate=None, ga
     what the forward call returned (its h, with want_stats), everything else what it was given.  Sums over the tokens (weights,
     biases, gate) come in fp32; the gradient of an argument that is None is None, and without dx those of the pre norm's are too."""
     import torch
-    T, n, dev, xt, ldh, ldy, ldg = _norm_operands(h, y, gate, gate_tokens, post, pre, None if dx is None else dx.dtype,
+    T, n, dev, xt, ldh, ldy, ldg = _norm_operands(h, y, gate, gate_tokens, None if dx is None else dx.dtype,
                                                   (post_weight, post_bias, pre_weight, pre_bias, gate))
     lddx = 0 if dx is None else _rows("dx", dx, T, n, dev, xt)
     lddho = 0 if dh is None else _rows("dh", dh, T, n, dev, h.dtype)

@@ -206,11 +206,12 @@ template <int M, int NT, int AT, int TT, int WAVES>
 static int launch_few_cfg(const I8FewArgs& a, int64_t R64, hipStream_t st) {
   constexpr int CS = M <= 8 ? 2 : 1, PITCH = CS * M * 16 + (M % 2 ? 8 : 16);
   auto kern = spmm_i8_few_kernel<M, NT, AT, TT, WAVES>;
-  if (int rc = allow_big_lds((const void*)kern, "hipFuncSetAttribute(spmm_i8_few)")) return rc;
   const int tp = (int)(a.T < TT ? a.T : TT) | 1;
-  const size_t xs = (size_t)WAVES * TT * PITCH, sums = (size_t)WAVES * 32 * AT * tp * 4;
+  const size_t xs = (size_t)WAVES * TT * PITCH, sums = (size_t)WAVES * 32 * AT * tp * 4, lds = xs > sums ? xs : sums;
+  if (lds > 64 * 1024)
+    if (int rc = allow_big_lds((const void*)kern, "hipFuncSetAttribute(spmm_i8_few)")) return rc;
   static_assert((size_t)WAVES * TT * PITCH <= 160 * 1024 && (size_t)WAVES * 32 * AT * (TT | 1) * 4 <= 160 * 1024, "LDS of a compute unit");
-  hipLaunchKernelGGL(kern, dim3((unsigned)(AT == 1 ? 2 * R64 : R64), (unsigned)((a.T + TT - 1) / TT)), dim3(64 * WAVES), xs > sums ? xs : sums, st, a, tp);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(AT == 1 ? 2 * R64 : R64), (unsigned)((a.T + TT - 1) / TT)), dim3(64 * WAVES), lds, st, a, tp);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) { set_hip_error(e, "spmm_i8_few_kernel"); return VNM_ERR_HIP; }
   return VNM_OK;

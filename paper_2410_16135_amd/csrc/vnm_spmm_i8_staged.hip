@@ -13,7 +13,9 @@
 // loads of weights; of a compute unit with 8 such waves that is 512 cycles of its matrix cores, 512 of LDS and 480 of the
 // 64 bytes per cycle that reach it (M = 5): balanced, so the loop is written in assembly with explicit waits, in which
 // younger requests stay in flight (compiled code drains all of them at each use).
+#include <type_traits>
 #include "vnm_i8.h"
+#include "vnm_i8_rules.h"
 
 namespace vnm {
 
@@ -424,41 +426,49 @@ spmm_i8_staged_kernel(const I8StagedArgs a) {
   float sx[BE];
 #pragma unroll
   for (int j = 0; j < BE; ++j) sx[j] = scales[128 + j * 32 + tokl];
-  const bool half = a.e.y_dtype != VNM_F32, lds_turn = half && a.wide_store;
+  const bool half = a.e.y_dtype != VNM_F32;
+  // (type and bias are decided once: decided at each of the 128 values of a lane they cost a third of this part's time)
+  auto each = [&](auto has_bias, auto&& take) {
 #pragma unroll
-  for (int i = 0; i < AT; ++i)
+    for (int i = 0; i < AT; ++i)
 #pragma unroll
-    for (int jq = 0; jq < 4; ++jq) {
-      const int row = i * 32 + 8 * jq + 4 * hB;          // of the lane's four channels
-      const int64_t o = r * 64 + row;
-      const f4v sw = *(const f4v*)(scales + row), bias = *(const f4v*)(scales + 64 + row);
+      for (int jq = 0; jq < 4; ++jq) {
+        const int row = i * 32 + 8 * jq + 4 * hB;        // of the lane's four channels
+        const f4v sw = *(const f4v*)(scales + row), bias = *(const f4v*)(scales + 64 + row);
 #pragma unroll
-      for (int j = 0; j < BE; ++j) {
-        float v[4];
+        for (int j = 0; j < BE; ++j) {
+          float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = i8_result(acc[i][j][4 * jq + e], sw[e], sx[j], a.e.bias, bias[e]);
-        if (lds_turn) {
-          // 16-bit results are turned around in LDS, from 4 channels of a token per lane to whole runs of a token's row
-          u2v pk;
-          if (a.e.y_dtype == VNM_F16) {
-            typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-            pk = __builtin_bit_cast(u2v, (h4){(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]});
-          } else
-            pk = (u2v){bf16_bits(v[0]) | (unsigned)bf16_bits(v[1]) << 16, bf16_bits(v[2]) | (unsigned)bf16_bits(v[3]) << 16};
-          *(u2v*)(ep + (size_t)(j * 32 + tokl) * EP + (i * 32 + 8 * jq + 4 * hB) * 2) = pk;
-        } else {
-          const int64_t t = t_wave + j * 32 + tokl;
-          if (t >= a.T) continue;
-          if (!half && a.vec_store && o + 3 < a.out)
-            __builtin_nontemporal_store((f4v){v[0], v[1], v[2], v[3]}, (f4v*)((float*)a.e.Y + t * a.e.ldy + o));
-          else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) if (o + e < a.out) i8_store(a.e, t, o + e, v[e]);
-          }
+          for (int e = 0; e < 4; ++e) v[e] = i8_result(acc[i][j][4 * jq + e], sw[e], sx[j], decltype(has_bias)::value, bias[e]);
+          take(row, j, v);
         }
       }
-    }
-  if (!lds_turn) return;
+  };
+  auto either = [&](auto&& take) { if (a.e.bias) each(std::true_type{}, take); else each(std::false_type{}, take); };
+  if (!(half && a.wide_store)) {
+    either([&](int row, int j, const float (&v)[4]) {
+      const int64_t t = t_wave + j * 32 + tokl, o = r * 64 + row;
+      if (t >= a.T) return;
+      if (!half && a.vec_store && o + 3 < a.out)
+        __builtin_nontemporal_store((f4v){v[0], v[1], v[2], v[3]}, (f4v*)((float*)a.e.Y + t * a.e.ldy + o));
+      else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (o + e < a.out) i8_store(a.e, t, o + e, v[e]);
+      }
+    });
+    return;
+  }
+  // 16-bit results are turned around in LDS, from 4 channels of a token per lane to whole runs of a token's row
+  auto turn = [&](int row, int j, u2v pk) { *(u2v*)(ep + (size_t)(j * 32 + tokl) * EP + row * 2) = pk; };
+  if (a.e.y_dtype == VNM_F16)
+    either([&](int row, int j, const float (&v)[4]) {
+      typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+      turn(row, j, __builtin_bit_cast(u2v, (h4){(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]}));
+    });
+  else
+    either([&](int row, int j, const float (&v)[4]) {
+      turn(row, j, (u2v){bf16_bits(v[0]) | (unsigned)bf16_bits(v[1]) << 16, bf16_bits(v[2]) | (unsigned)bf16_bits(v[3]) << 16});
+    });
   const int ch = lane & 7, tl = lane >> 3;
   unsigned short* Y = (unsigned short*)a.e.Y;
 #pragma unroll
@@ -535,7 +545,7 @@ int launch_spmm_i8_staged(const void* staged, int64_t T, const void* packed, con
   a.vec_store = !half && e.ldy % 4 == 0 && ((uintptr_t)e.Y & 15) == 0;
   const int64_t tiles = (T + kTokTile - 1) / kTokTile;
   const bool dual = packed_tables(d.V) == 2;
-  const bool wide = a.R >= 8 && tiles * ((a.R + 7) / 8) > 128;
+  const bool wide = i8_staged_wide(tiles, a.R);
   return dual ? launch_staged<true>(a, d.M, wide, st) : launch_staged<false>(a, d.M, wide, st);
 }
 
