@@ -433,6 +433,22 @@ int vnm_spmm_i8(const void* Q, int64_t T, int64_t ldq, const void* scale_x, cons
 int vnm_spmm_i8_workspace_bytes(int64_t T, int64_t out, int64_t in, int V, int N, int M, int64_t* bytes);
 
 /*
+ * The two halves of the many-token product as separate calls, for layers that read the same activations
+ * (q, k and v, or gate and up): vnm_stage_q re-lays Q once, vnm_spmm_i8_staged multiplies.  Same bits as
+ * vnm_spmm_i8, which is the better call up to about 300 tokens.
+ *   staged   dev, 256-byte aligned, vnm_stage_q_bytes(T, in, M) bytes; depends on T, in and M only.  That
+ *            size includes images that the product's look-ahead reads (and never uses), and a smaller
+ *            buffer is refused (VNM_ERR_WORKSPACE)
+ *   Q        as for the matrix-core kernels of vnm_spmm_i8 (ldq % 16 == 0, 16-byte aligned, M <= 16);
+ *            otherwise VNM_ERR_UNSUPPORTED
+ */
+int vnm_stage_q_bytes(int64_t T, int64_t in, int M, int64_t* bytes);
+int vnm_stage_q(const void* Q, int64_t T, int64_t ldq, int64_t in, int M, void* staged, int64_t staged_bytes, void* stream);
+int vnm_spmm_i8_staged(const void* staged, int64_t staged_bytes, int64_t T, const void* scale_x, const void* packed,
+                       const void* scale_w, int64_t out, int64_t in, int V, int N, int M, const void* bias, void* Y,
+                       int64_t ldy, int y_dtype, void* stream);
+
+/*
  * What stands between two blocks: the norm after a block, its gate, the residual addition, and the norm
  * in front of the next block, in one pass over the tokens:
  *   p[t]  = norm_post(y[t])                         the block's output, normalised unless post is VNM_NORM_NONE

@@ -13,5 +13,6 @@ from .binding import (  # noqa: F401
     vnm_mask_diversity_log, vnm_select_vm, vnm_spmm_fused, vnm_fold_permutations, vnm_permutation_search,
     vnm_permutation_gain, vnm_retained_score, vnm_lora_merge, vnm_refresh_mask, PATH_AUTO, PATH_GENERIC, PATH_SMFMAC,
     CompressedI8, vnm_quantize_x, vnm_quantize_compressed, vnm_pack_i8, vnm_spmm_i8, vnm_spmm_i8_workspace_bytes,
+    vnm_stage_q, vnm_spmm_i8_staged,
     ResidualNorm, ResidualNormGrads, vnm_residual_norm, vnm_residual_norm_backward,
 )

@@ -140,11 +140,14 @@ def load_library():
     lib.vnm_pack_i8.argtypes = [vp, vp, vp, i64, i64, ci, ci, ci, vp, vp]
     lib.vnm_spmm_i8.argtypes = [vp, i64, i64, vp, vp, vp, vp, vp, vp, i64, i64, ci, ci, ci, vp, vp, i64, ci, ci, vp, i64, vp]
     lib.vnm_spmm_i8_workspace_bytes.argtypes = [i64, i64, i64, ci, ci, ci, ctypes.POINTER(i64)]
+    lib.vnm_stage_q_bytes.argtypes = [i64, i64, ci, ctypes.POINTER(i64)]
+    lib.vnm_stage_q.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp]
+    lib.vnm_spmm_i8_staged.argtypes = [vp, i64, i64, vp, vp, vp, i64, i64, ci, ci, ci, vp, vp, i64, ci, vp]
     lib.vnm_residual_norm.argtypes = [vp, vp]
     lib.vnm_residual_norm_backward.argtypes = [vp, vp, i64, vp]
     lib.vnm_residual_norm_backward_workspace_bytes.argtypes = [i64, i64, i64, ctypes.POINTER(i64)]
     for f in (lib.vnm_quantize_x, lib.vnm_i8_packed_bytes, lib.vnm_quantize_compressed, lib.vnm_pack_i8, lib.vnm_spmm_i8,
-              lib.vnm_spmm_i8_workspace_bytes, lib.vnm_residual_norm, lib.vnm_residual_norm_backward,
+              lib.vnm_spmm_i8_workspace_bytes, lib.vnm_stage_q_bytes, lib.vnm_stage_q, lib.vnm_spmm_i8_staged, lib.vnm_residual_norm, lib.vnm_residual_norm_backward,
               lib.vnm_residual_norm_backward_workspace_bytes):
         f.restype = ci
     lib.vnm_status_string.argtypes = [ci]
@@ -805,6 +808,38 @@ def vnm_spmm_i8(Q, scale, c: CompressedI8, bias=None, N: int = 2, out_dtype=None
         0 if workspace is None else workspace.numel(), _raw_stream(dev))
     if status:
         _check(status, "vnm_spmm_i8")
+    return Y
+
+
+def vnm_stage_q(Q, M: int, staged=None):
+    """Re-lay int8 activations Q [T x in] for the many-token kernel; returns the staged uint8 tensor (reusable by every int8 layer
+    with the same `in` and M)."""
+    import torch
+    assert Q.is_cuda and Q.dim() == 2
+    T, inn = Q.shape
+    dev = Q.device
+    ldq = _rows("Q", Q, T, inn, dev, torch.int8)
+    if T <= 1:
+        ldq = (inn + 15) // 16 * 16              # (one row: whatever the view's stride)
+    b = ctypes.c_int64(0)
+    _check(load_library().vnm_stage_q_bytes(T, inn, M, ctypes.byref(b)), "vnm_stage_q_bytes")
+    if staged is None:
+        staged = torch.empty(max(b.value, 1), dtype=torch.uint8, device=dev)
+    _launch("vnm_stage_q", load_library().vnm_stage_q, dev, Q.data_ptr(), T, ldq, inn, M, staged.data_ptr(), staged.numel())
+    return staged
+
+
+def vnm_spmm_i8_staged(staged, scale, c: CompressedI8, bias=None, N: int = 2, out_dtype=None, Y=None):
+    """vnm_spmm_i8 on activations staged by vnm_stage_q; `scale` fp32 [T] as there."""
+    import torch
+    dev, T = staged.device, scale.shape[0]
+    assert staged.is_cuda and staged.dtype == torch.uint8 and staged.is_contiguous() and c.packed is not None and c.packed.device == dev
+    if Y is None:
+        Y = torch.empty((T, c.out), dtype=out_dtype or torch.float16, device=dev)
+    ldy = _rows("Y", Y, T, c.out, dev)
+    _launch("vnm_spmm_i8_staged", load_library().vnm_spmm_i8_staged, dev, staged.data_ptr(), staged.numel(), T,
+            _vector("scale", scale, T, dev, torch.float32), c.packed.data_ptr(), c.scale.data_ptr(), c.out, c.inn, c.V, N, c.M,
+            _vector("bias", bias, c.out, dev, torch.float16), Y.data_ptr(), ldy, _dtype_code(Y.dtype))
     return Y
 
 

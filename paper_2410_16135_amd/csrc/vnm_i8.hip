@@ -198,3 +198,40 @@ extern "C" int vnm_spmm_i8(const void* Q, int64_t T, int64_t ldq, const void* sc
   }
   return launch_spmm_i8_triple(Q, T, ldq, qvalues, meta, colidx, d, e, (hipStream_t)stream);
 }
+
+extern "C" int vnm_stage_q_bytes(int64_t T, int64_t in, int M, int64_t* bytes) {
+  if (!bytes) return VNM_ERR_NULL;
+  if (in <= 0 || T < 0) return VNM_ERR_SHAPE;
+  if (M < 4 || M > 16) return VNM_ERR_UNSUPPORTED;
+  *bytes = staged_q_bytes(T, make_dims(64, in, 64, M));            // (the layout depends on in and M only)
+  return VNM_OK;
+}
+
+extern "C" int vnm_stage_q(const void* Q, int64_t T, int64_t ldq, int64_t in, int M, void* staged, int64_t staged_bytes, void* stream) {
+  if (T != 0 && (!Q || !staged)) return VNM_ERR_NULL;
+  if (in <= 0 || T < 0 || ldq < in) return VNM_ERR_SHAPE;
+  if (M < 4 || M > 16 || ldq % 16 != 0 || ((uintptr_t)Q & 15)) return VNM_ERR_UNSUPPORTED;
+  if (T == 0) return VNM_OK;
+  const Dims d = make_dims(64, in, 64, M);
+  if (staged_bytes < staged_q_bytes(T, d)) return VNM_ERR_WORKSPACE;
+  if ((uintptr_t)staged & 255) return VNM_ERR_ALIGN;
+  return launch_stage_q(Q, T, ldq, d, staged, (hipStream_t)stream);
+}
+
+extern "C" int vnm_spmm_i8_staged(const void* staged, int64_t staged_bytes, int64_t T, const void* scale_x, const void* packed,
+                                  const void* scale_w, int64_t out, int64_t in, int V, int N, int M, const void* bias, void* Y,
+                                  int64_t ldy, int y_dtype, void* stream) {
+  if (!packed || !scale_w || (T != 0 && (!staged || !scale_x || !Y))) return VNM_ERR_NULL;
+  if (int rc = check_pattern(out, in, V, N, M)) return rc;
+  if (T < 0 || ldy < out) return VNM_ERR_SHAPE;
+  if (!dtype_ok(y_dtype) || !has_packed(V, M)) return VNM_ERR_UNSUPPORTED;
+  if (((uintptr_t)staged & 255) || ((uintptr_t)packed & 255) || ((uintptr_t)Y & dtype_mask(y_dtype)) || ((uintptr_t)scale_x & 3) ||
+      ((uintptr_t)scale_w & 3) || ((uintptr_t)bias & 1))
+    return VNM_ERR_ALIGN;
+  const Dims d = make_dims(out, in, V, M);
+  if (!i8_sums_fit(d)) return VNM_ERR_UNSUPPORTED;
+  if (T == 0) return VNM_OK;
+  if (staged_bytes < staged_q_bytes(T, d)) return VNM_ERR_WORKSPACE;
+  const I8Epilogue e{(const float*)scale_x, (const float*)scale_w, (const _Float16*)bias, Y, ldy, y_dtype};
+  return launch_spmm_i8_staged(staged, T, packed, d, e, (hipStream_t)stream);
+}

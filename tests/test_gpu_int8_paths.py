@@ -42,3 +42,37 @@ def test_product_paths_and_strides_agree(T):
         assert same(view, ref.product(q, sx, dense, sw, bias, dtype)), (dtype, ld, first)
         view.fill_(42.0)
         assert bool((buf == 42.0).all())
+
+
+@pytest.mark.parametrize("T", [1, 63, 128, 129, 700])
+@pytest.mark.parametrize("inn,M", [(128, 4), (333, 5), (1030, 8), (600, 16)])
+def test_shared_staging(inn, M, T):
+    """Two layers of other widths, row blocks, types and biases on activations that are staged once."""
+    staged = None
+    for out, V, dtype in ((70, 64, "fp16"), (600, 32, "bf16"), (130, 128, "fp32")):
+        c, q, sx, sw, bias, dense, Q, SX = make(out, inn, V, M, T, 17)
+        if staged is None:
+            first, staged = (q, sx, SX), vnm.vnm_stage_q(Q, M)
+        b = bias if V != 32 else None
+        got = vnm.vnm_spmm_i8_staged(staged, first[2], c, bias=None if b is None else torch.from_numpy(b).to(DEV), out_dtype=ref.TYPES[dtype])
+        assert same(got, ref.product(first[0], first[1], dense, sw, b, dtype)), (out, V)
+
+
+def test_shared_staging_buffer_too_small():
+    c, q, sx, sw, bias, dense, Q, SX = make(128, 256, 64, 8, 200, 3)
+    staged = vnm.vnm_stage_q(Q, 8)
+    for call in (lambda: vnm.vnm_stage_q(Q, 8, staged=staged[:-256]), lambda: vnm.vnm_spmm_i8_staged(staged[:-256], SX, c)):
+        with pytest.raises(vnm.VnmError, match="workspace"):
+            call()
+
+
+def test_staging_reads_no_row_past_the_last():
+    """The activations end with their storage: rows of 16-byte pieces of which the last is cut."""
+    T, inn = 150, 1000 - 3
+    c, q, sx, sw, bias, dense, Q, SX = make(192, inn, 64, 5, T, 23)
+    buf = torch.zeros((T - 1) * 1008 + inn + 11, dtype=torch.int8, device=DEV)        # (up to the piece's end)
+    view = buf[:(T - 1) * 1008 + inn].as_strided((T, inn), (1008, 1))
+    view.copy_(Q)
+    want = ref.product(q, sx, dense, sw, None, "fp16")
+    assert same(vnm.vnm_spmm_i8(view, SX, c), want)
+    assert same(vnm.vnm_spmm_i8_staged(vnm.vnm_stage_q(view, 5), SX, c), want)

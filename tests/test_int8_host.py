@@ -75,6 +75,35 @@ def test_pack_and_sizes(lib):
     assert lib.vnm_spmm_i8_workspace_bytes(0, 128, 128, 64, 2, 8, ctypes.byref(b)) == OK and b.value >= 0
 
 
+def test_staging_refusals(lib):
+    b = ctypes.c_int64(-1)
+    q = lib.vnm_stage_q_bytes
+    assert q(4, 128, 8, None) == NULL and q(-1, 128, 8, ctypes.byref(b)) == SHAPE and q(4, 0, 8, ctypes.byref(b)) == SHAPE
+    assert q(4, 128, 3, ctypes.byref(b)) == UNSUPPORTED and q(4, 128, 17, ctypes.byref(b)) == UNSUPPORTED
+    # a tile of 128 tokens and the look-ahead: 16 M rows of 144 bytes, whole KiB, per step of 16 M columns
+    assert q(4, 128, 8, ctypes.byref(b)) == OK and b.value == (1 + 5) * 18 * 1024
+    need, st = b.value, lib.vnm_stage_q
+    assert st(None, 0, 128, 128, 8, None, 0, None) == OK
+    assert st(None, 4, 128, 128, 8, G, need, None) == NULL and st(G, 4, 128, 128, 8, None, need, None) == NULL
+    assert st(G, 4, 127, 128, 8, G, need, None) == SHAPE and st(G, 4, 136, 128, 8, G, need, None) == UNSUPPORTED
+    assert st(P(0x10008), 4, 128, 128, 8, G, need, None) == UNSUPPORTED and st(G, 4, 128, 128, 17, G, need, None) == UNSUPPORTED
+    assert st(G, 4, 128, 128, 8, G, need - 1, None) == WORKSPACE and st(G, 4, 128, 128, 8, P(0x10080), need, None) == ALIGN
+
+    def product(**over):
+        a = dict(staged=G, bytes=need, T=4, sx=G, packed=G, sw=G, out=128, inn=128, V=64, N=2, M=8, bias=None, Y=G, ldy=128, y_dtype=0, stream=None)
+        a.update(over)
+        return lib.vnm_spmm_i8_staged(*a.values())
+
+    assert product(T=0, staged=None, bytes=0, sx=None, Y=None) == OK
+    for name in ("staged", "sx", "packed", "sw", "Y"):
+        assert product(**{name: None}) == NULL, name
+    assert product(T=-1) == SHAPE and product(ldy=127) == SHAPE and product(out=0) == SHAPE
+    assert product(y_dtype=4) == UNSUPPORTED and product(V=16) == UNSUPPORTED and product(M=17) == UNSUPPORTED
+    assert product(inn=65536 * 8, bytes=1 << 60) == UNSUPPORTED and product(bytes=need - 1) == WORKSPACE
+    for name, at in (("staged", 0x10010), ("packed", 0x10080), ("sx", 0x10002), ("sw", 0x10002), ("bias", 0x10001), ("Y", 0x10001)):
+        assert product(**{name: P(at)}) == ALIGN, name
+
+
 def _forward_args(**over):
     f = dict(T=4, n=64, h_dtype=0, x_dtype=0, post=0, pre=1, post_eps=1e-5, pre_eps=1e-5, residual_scale=1.0, gate_tokens=0, h=0x10000,
              ldh=64, ldy=64, ldg=64, h_out=0x20000, x=0x30000, ldho=64, ldx=64, ldq=64)
