@@ -758,9 +758,11 @@ def vnm_pack_i8(c: CompressedI8, N: int = 2) -> CompressedI8:
     """Fills c.packed from the triple (allocated where it is None and this V, M has one)."""
     import torch
     _check_triple(c.values, torch.int8, c, N)
+    fresh = _i8_packed(c, N)
     if c.packed is None:
-        c.packed = _i8_packed(c, N)
+        c.packed = fresh
     if c.packed is not None:
+        assert fresh is not None and c.packed.device == c.values.device and c.packed.numel() >= fresh.numel(), "packed"
         _launch("vnm_pack_i8", load_library().vnm_pack_i8, c.values.device, _ptr(c.values), _ptr(c.meta), _ptr(c.colidx), c.out,
                 c.inn, c.V, N, c.M, _ptr(c.packed))
     return c

@@ -43,6 +43,8 @@ constexpr int kImagePitchI8 = kTokTile + 16;
 inline int64_t i8_image_bytes(int M) { return ((int64_t)16 * M * kImagePitchI8 + 1023) / 1024 * 1024; }
 int64_t staged_q_bytes(int64_t T, const Dims& d);
 
+constexpr int64_t kI8MaxRowPitch = 1 << 24;    // of activations: the few-token kernel's offsets within 64 rows have 31 bits
+
 // No sum may leave 32 bits, whatever the int8 values (-128 included)
 inline bool i8_sums_fit(const Dims& d) { return 2 * d.B <= (0x7FFFFFFFll >> 14); }
 

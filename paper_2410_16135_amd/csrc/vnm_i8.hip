@@ -186,7 +186,8 @@ extern "C" int vnm_spmm_i8(const void* Q, int64_t T, int64_t ldq, const void* sc
   const Dims d = make_dims(out, in, V, M);
   if (!i8_sums_fit(d)) return VNM_ERR_UNSUPPORTED;
   if (T == 0) return VNM_OK;
-  const bool matrix = packed && has_packed(V, M) && ldq % 16 == 0 && ((uintptr_t)Q & 15) == 0;
+  // (rows so far apart that 64 of them leave 31 bits are the kernel on the triple's business)
+  const bool matrix = packed && has_packed(V, M) && ldq % 16 == 0 && ((uintptr_t)Q & 15) == 0 && ldq <= kI8MaxRowPitch;
   if (path == VNM_PATH_SMFMAC && !matrix) return VNM_ERR_UNSUPPORTED;
   const I8Epilogue e{(const float*)scale_x, (const float*)scale_w, (const _Float16*)bias, Y, ldy, y_dtype};
   if (path != VNM_PATH_GENERIC && matrix) {
@@ -210,7 +211,7 @@ extern "C" int vnm_stage_q_bytes(int64_t T, int64_t in, int M, int64_t* bytes) {
 extern "C" int vnm_stage_q(const void* Q, int64_t T, int64_t ldq, int64_t in, int M, void* staged, int64_t staged_bytes, void* stream) {
   if (T != 0 && (!Q || !staged)) return VNM_ERR_NULL;
   if (in <= 0 || T < 0 || ldq < in) return VNM_ERR_SHAPE;
-  if (M < 4 || M > 16 || ldq % 16 != 0 || ((uintptr_t)Q & 15)) return VNM_ERR_UNSUPPORTED;
+  if (M < 4 || M > 16 || ldq % 16 != 0 || ((uintptr_t)Q & 15) || in > 0x7FFFFFFF) return VNM_ERR_UNSUPPORTED;
   if (T == 0) return VNM_OK;
   const Dims d = make_dims(64, in, 64, M);
   if (staged_bytes < staged_q_bytes(T, d)) return VNM_ERR_WORKSPACE;

@@ -45,6 +45,7 @@ inline double i8_staged_us(int64_t T, int64_t R64, int64_t in, int64_t S) {
 }
 inline bool i8_takes_few(int64_t T, int64_t R64, int64_t in, int64_t S, int M) {
   if (T <= 128) return true;
+  if (T > 4 * 65535) return false;                          // (its grid)
   return i8_few_us(i8_few_shape(T, R64, S, M), T, R64, S, M) < i8_staged_us(T, R64, in, S);
 }
 

@@ -235,7 +235,8 @@ static int launch_few_m(const I8FewArgs& a, const Dims& d, hipStream_t st) {
 int launch_spmm_i8_few(const void* Q, int64_t T, int64_t ldq, const void* packed, const Dims& d, const I8Epilogue& e, hipStream_t st) {
   const I8Layout l = i8_layout(d);
   const unsigned char* p = (const unsigned char*)packed;
-  if (2 * packed_row_blocks(d) > 0x7FFFFFFF || (T + 3) / 4 > 65535 || i8_steps(d) * 16 * d.M > 0x7FFFFFFF || 64 * ldq + i8_steps(d) * 16 * d.M > 0x7FFFFFFF) return VNM_ERR_UNSUPPORTED;
+  // (ldq <= kI8MaxRowPitch, and i8_sums_fit bounds a row at 2^20 channels: 64 rows and a step stay in 31 bits)
+  if (2 * packed_row_blocks(d) > 0x7FFFFFFF || (T + 3) / 4 > 65535 || ldq > kI8MaxRowPitch) return VNM_ERR_UNSUPPORTED;
   const I8FewArgs a{(const unsigned char*)Q, T, ldq, (int)d.in, p, p + l.pidx_off, p + l.psel_off, d.out, (unsigned)i8_steps(d), e};
   switch (d.M) {
     case 4: return launch_few_m<4>(a, d, st);
