@@ -16,8 +16,10 @@ namespace vnm {
 //   pcol  u32  [R64][S][16 roles][NT]            raw column within the step (0 .. 16 M - 1) of the row that lane role
 //                                                (h, r) = 8 h + r addresses in transposing read i, at bits 8 i: kept
 //                                                column r mod 4 of block 8 h + 2 i + r / 4
-//   psel  u32  [R64][S][NT][NSEL][16 blocks]     byte selectors: the 4 kept columns of a block as bytes of the dwords that
-//                                                hold its M raw columns (8 bytes per selector; 0x0c selects zero)
+//   psel  u32  [R64][S][NT][NSEL][2 h][4]        byte selectors: the 4 kept columns of a block as bytes of the dwords that
+//                                                hold its M raw columns (8 bytes per selector; 12 selects zero), 4 bits
+//                                                each: dword i has block 8 h + 2 i in the low halves of its bytes, the
+//                                                next block in the high ones
 inline int64_t i8_steps(const Dims& d) { return (d.B + 15) / 16; }
 constexpr int i8_selectors(int M) {            // 8-byte pairs of dwords that a block of a lane's run can reach into
   int most = 0;
@@ -34,7 +36,7 @@ inline I8Layout i8_layout(const Dims& d) {
   l.pidx_off = up(rs * 2048);
   l.pcol_off = l.pidx_off + up(rs * 512);
   l.psel_off = l.pcol_off + up(rs * 64 * nt);
-  l.total = l.psel_off + up(rs * 64 * nt * i8_selectors(d.M)) + kI8Slack;
+  l.total = l.psel_off + up(rs * 32 * nt * i8_selectors(d.M)) + kI8Slack;
   return l;
 }
 // Staged activations: an image per (tile of kTokTile tokens, K step), 16 M rows [raw column][token] 160 bytes apart -- 8 rows that

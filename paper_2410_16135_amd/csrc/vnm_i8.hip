@@ -5,7 +5,7 @@
 namespace vnm {
 
 // ---------------------------------------------------------------- pack
-// One thread per (64-row block, step, tile, lane) for the A operand, and one per entry of the two column tables.
+// One thread per (64-row block, step, tile, lane) for the A operand, and one per dword of the two column tables.
 __global__ void __launch_bounds__(256)
 pack_i8_kernel(const unsigned char* __restrict__ qvalues, const unsigned char* __restrict__ meta,
                const unsigned char* __restrict__ colidx, int64_t in, int V, int M, int64_t R, int64_t B, int64_t RS, int64_t S,
@@ -44,32 +44,34 @@ pack_i8_kernel(const unsigned char* __restrict__ qvalues, const unsigned char* _
     pidx[rs * 128 + lane * 2 + at] = idx;
   }
   if (gid < RS * 16 * NT) {
-    {
-      const int t = (int)(gid % NT), role = (int)(gid / NT % 16), h = role >> 3, r = role & 7;
-      const int64_t rs = gid / NT / 16, s = rs % S, rb = ((rs / S) * 64 + t * 32) / V;
-      unsigned o = 0;
+    const int t = (int)(gid % NT), role = (int)(gid / NT % 16), h = role >> 3, r = role & 7;
+    const int64_t rs = gid / NT / 16, s = rs % S, rb = ((rs / S) * 64 + t * 32) / V;
+    unsigned o = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int blk = 8 * h + 2 * i + (r >> 2);
-        const int64_t b = s * 16 + blk;
-        const unsigned c = b < B && rb < R ? colidx[(rb * B + b) * 4 + (r & 3)] : (unsigned)(r & 3);
-        o |= (unsigned)(blk * M + (int)c) << (8 * i);
-      }
-      pcol[gid] = o;
+    for (int i = 0; i < 4; ++i) {
+      const int blk = 8 * h + 2 * i + (r >> 2);
+      const int64_t b = s * 16 + blk;
+      const unsigned c = b < B && rb < R ? colidx[(rb * B + b) * 4 + (r & 3)] : (unsigned)(r & 3);
+      o |= (unsigned)(blk * M + (int)c) << (8 * i);
     }
-    {
-      const int blk = (int)(gid % 16), t = (int)(gid / 16 % NT);
-      const int64_t rs = gid / 16 / NT, s = rs % S, rb = ((rs / S) * 64 + t * 32) / V, b = s * 16 + blk;
-      const int first = (M * (blk & 7)) & 3;               // byte of the block's first column in its first dword
-      for (int w = 0; w < nsel; ++w) {
-        unsigned sel = 0;
+    pcol[gid] = o;
+  }
+  if (gid < RS * 8 * NT) {                                 // two blocks of a lane half's run
+    const int i = (int)(gid & 3), h = (int)(gid >> 2) & 1, t = (int)(gid / 8 % NT);
+    const int64_t rs = gid / 8 / NT, s = rs % S, rb = ((rs / S) * 64 + t * 32) / V;
+    for (int w = 0; w < nsel; ++w) {
+      unsigned sel = 0;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int d = 2 * i + e, first = (M * d) & 3;      // byte of the block's first column in its first dword
+        const int64_t b = s * 16 + 8 * h + d;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int at = first + (b < B && rb < R ? (int)colidx[(rb * B + b) * 4 + k] : k) - 8 * w;
-          sel |= (unsigned)(at >= 0 && at < 8 ? at : 0x0c) << (8 * k);
+          sel |= (unsigned)(at >= 0 && at < 8 ? at : 12) << (8 * k + 4 * e);
         }
-        psel[((rs * NT + t) * nsel + w) * 16 + blk] = sel;
       }
+      psel[(((rs * NT + t) * nsel + w) * 2 + h) * 4 + i] = sel;
     }
   }
 }

@@ -18,7 +18,8 @@ struct I8FewArgs {
 };
 
 // The 4 kept columns of the 8 blocks of a lane's run, from its raw dwords: a byte permutation per 8 bytes that a block can reach
-// into (selectors of bytes elsewhere give zero).
+// into (selectors of bytes elsewhere give zero).  Selectors come 4 bits each, two blocks to a dword: 16 bytes per lane instead
+// of 32 are a load less per step for one and a half instructions more per block.
 template <int M>
 __device__ __forceinline__ i8v i8_gather(const unsigned (&x)[2 * M], const u4v* sel) {
   constexpr int NSEL = i8_selectors(M);
@@ -29,7 +30,7 @@ __device__ __forceinline__ i8v i8_gather(const unsigned (&x)[2 * M], const u4v* 
     unsigned v = 0;
 #pragma unroll
     for (int w = 0; w < NSEL; ++w) {
-      const unsigned s = sel[2 * w + (d >> 2)][d & 3];
+      const unsigned two = sel[w][d >> 1], s = (d & 1 ? two >> 4 : two) & 0x0f0f0f0fu;
       const int lo = first + 2 * w, hi = lo + 1;
       if (lo < 2 * M) {
         const unsigned p = __builtin_amdgcn_perm(hi < 2 * M ? x[hi] : 0u, x[lo], s);
@@ -102,7 +103,7 @@ spmm_i8_few_kernel(const I8FewArgs a, const int tp) {
       }
     }
   };
-  struct Slot { u4v w[AT]; unsigned idx[AT]; u4v sel[TABLES * 2 * NSEL]; };
+  struct Slot { u4v w[AT]; unsigned idx[AT]; u4v sel[TABLES * NSEL]; };
   auto load_w = [&](Slot& o, unsigned s) {
     s = s < S ? s : S - 1;                         // (beyond the wave's range: not used)
     const size_t rs = rs0 + s;
@@ -116,10 +117,7 @@ spmm_i8_few_kernel(const I8FewArgs a, const int tp) {
     for (int t = 0; t < TABLES; ++t)
 #pragma unroll
       for (int k = 0; k < NSEL; ++k)
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-          o.sel[(t * NSEL + k) * 2 + q] =
-              *(const u4v*)(a.psel + ((rs * NT + (AT == 2 ? t : NT == 2 ? at : 0)) * NSEL + k) * 64 + q * 16 + (unsigned)(h * 32));
+        o.sel[t * NSEL + k] = *(const u4v*)(a.psel + ((rs * NT + (AT == 2 ? t : NT == 2 ? at : 0)) * NSEL + k) * 32 + (unsigned)(h * 16));
   };
   i16v acc[AT][G];
 #pragma unroll
@@ -148,7 +146,7 @@ spmm_i8_few_kernel(const I8FewArgs a, const int tp) {
       i8v b = i8_gather<M>(x, o.sel);
 #pragma unroll
       for (int i = 0; i < AT; ++i) {
-        if (TABLES == 2 && i == 1) b = i8_gather<M>(x, o.sel + 2 * NSEL);
+        if (TABLES == 2 && i == 1) b = i8_gather<M>(x, o.sel + NSEL);
         acc[i][g] = __builtin_amdgcn_smfmac_i32_32x32x64_i8(__builtin_bit_cast(i4v, o.w[i]), b, acc[i][g], (int)o.idx[i], 0, 0);
       }
     }
