@@ -36,9 +36,10 @@ def parse():
     ap.add_argument("--gpus", type=int, default=1)
     ap.add_argument("--steps", type=int, default=20)
     ap.add_argument("--warmup", type=int, default=3)
-    ap.add_argument("--workload", default="llama2_7b", choices=["llama2_7b", "deit_small", "deit_base", "single", "sweep"],
+    ap.add_argument("--workload", default="llama2_7b", choices=["llama2_7b", "deit_small", "deit_base", "single", "sweep", "int8_block"],
                     help="sweep: times vnm_spmm and vnm_prune_compress against the dense fp16 GEMM over the "
-                         "V x M x tokens grid on the two large Llama shapes and runs the (V, M) selection on it")
+                         "V x M x tokens grid on the two large Llama shapes and runs the (V, M) selection on it; int8_block: the "
+                         "layers of a Llama-2-7B block in 8 bits with the norms around them, against the same in 16 bits")
     ap.add_argument("--V", type=int, default=None)
     ap.add_argument("--M", type=int, default=None)
     ap.add_argument("--tokens", type=int, default=None)
@@ -139,6 +140,90 @@ def run_sweep(args):
                       "dense_baseline": (dense_desc + "; the faster of this and torch.matmul per point") if searched
                       else "UNTUNED: torch.matmul fp16 with default heuristics (" + dense_desc + ")",
                       "points": rows, "selected_vm_by_threshold": selection}))
+
+
+def run_int8_block(args):
+    """A Llama-2-7B block's V:N:M layers in 8 bits, with the norms in front of them and the quantization of what no norm
+    produces, against the same pass in 16 bits (not the default workload).  Attention and the activation function are not this
+    library's: their outputs are stood in for by v's and by gate's.  Both passes are replayed from HIP graphs in turn."""
+    import torch
+    import paper_2410_16135_amd as vnm
+    import synth_inputs as syn
+    dev = torch.device("cuda:0")
+    layers = syn.config_llama2_7b(args.V or 64, args.M or 5, tokens=args.tokens or 4096)
+    T, n, M = layers[0].tokens, layers[0].inn, layers[0].M
+    w16, w8 = {}, {}
+    for L in layers:
+        W, X = syn.layer_tensors(L, tokens=T if L.name == "q" else 1)
+        if L.name == "q":
+            h = torch.from_numpy(X).to(dev)
+        w16[L.name] = vnm.vnm_prune_compress(torch.from_numpy(W).to(dev), L.V, L.M)
+        w8[L.name] = vnm.vnm_quantize_compressed(w16[L.name])
+    norm = torch.ones(n, dtype=torch.float16, device=dev)
+    shared = vnm.vnm_spmm_i8_workspace_bytes(T, w8["q"]) > 0            # layers that read one input share its staging
+    # (the 16-bit products get workspaces of their own: a graph replays on them)
+    ws = {L.name: torch.empty(max(vnm.vnm_spmm_workspace_bytes(T, w16[L.name]), 256), dtype=torch.uint8, device=dev) for L in layers}
+
+    def products8(x, scale, names):
+        if shared and len(names) > 1:
+            staged = vnm.vnm_stage_q(x, M)
+            return [vnm.vnm_spmm_i8_staged(staged, scale, w8[k]) for k in names]
+        return [vnm.vnm_spmm_i8(x, scale, w8[k]) for k in names]
+
+    def products16(x, names):
+        if len(names) > 1 and vnm.vnm_spmm_kernel_choice(T, w16[names[0]], ws[names[0]].numel()) == vnm.KERNEL_STAGED:
+            staged = vnm.vnm_stage_x(x, M)
+            return [vnm.vnm_spmm_staged(staged, T, w16[k], scratch=ws[k]) for k in names]
+        return [vnm.vnm_spmm(x, w16[k], workspace=ws[k]) for k in names]
+
+    def block8():
+        a = vnm.vnm_residual_norm(h, pre="rms", pre_weight=norm, int8=True)
+        v = products8(a.x, a.scale, ["q", "k", "v"])[2]
+        y, = products8(*vnm.vnm_quantize_x(v), ["o"])
+        b = vnm.vnm_residual_norm(a.h, y, pre="rms", pre_weight=norm, int8=True)
+        g = products8(b.x, b.scale, ["gate", "up"])[0]
+        y, = products8(*vnm.vnm_quantize_x(g), ["down"])
+        return vnm.vnm_residual_norm(b.h, y, want_x=False).h
+
+    def block16():
+        a = vnm.vnm_residual_norm(h, pre="rms", pre_weight=norm)
+        v = products16(a.x, ["q", "k", "v"])[2]
+        y, = products16(v, ["o"])
+        b = vnm.vnm_residual_norm(a.h, y, pre="rms", pre_weight=norm)
+        g = products16(b.x, ["gate", "up"])[0]
+        y, = products16(g, ["down"])
+        return vnm.vnm_residual_norm(b.h, y, want_x=False).h
+
+    def captured(f):
+        f()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = f()
+        return g, out
+
+    def replay(g, k):
+        torch.cuda.synchronize()
+        t = time.perf_counter()
+        for _ in range(k):
+            g.replay()
+        torch.cuda.synchronize()
+        return (time.perf_counter() - t) / k
+    (g8, out8), (g16, out16) = captured(block8), captured(block16)
+    for g in (g8, g16):
+        replay(g, max(args.warmup, 1))
+    t8, t16 = [], []
+    for _ in range(4):
+        t8.append(replay(g8, args.steps))
+        t16.append(replay(g16, args.steps))
+    s8, s16 = sorted(t8)[len(t8) // 2], sorted(t16)[len(t16) // 2]
+    far = float((out8.double() - out16.double()).norm() / out16.double().norm())
+    print(json.dumps({
+        "metric": "Llama-2-7B block of V:N:M layers and norms in 8 bits", "value": T / s8, "unit": "tokens/s", "n_gpus": 1,
+        "steps": args.steps, "warmup": args.warmup, "ms_per_step": s8 * 1e3, "higher_is_better": True, "scaling": "weak",
+        "vs_baseline": None, "dtype": "int8", "data": "synthetic",
+        "fp16_ms_per_step": s16 * 1e3, "speedup_over_fp16": s16 / s8, "residual_stream_relative_difference": far,
+        "config": {"model": f"Llama-2-7B block, {layers[0].V}:2:{M}", "global_batch": 1, "seq_len": T, "parallelism": "none"}}))
 
 
 DENSE_HELPER = os.path.join(ROOT, "bench_dense_gemm")
@@ -327,6 +412,9 @@ def main():
     import paper_2410_16135_amd as vnm
     import synth_inputs as syn
 
+    if args.workload == "int8_block":
+        run_int8_block(args)
+        return
     if args.workload == "sweep":
         run_sweep(args)
         return
