@@ -673,6 +673,13 @@ def _vector(name, t, n, device, dtype):
     return t.data_ptr()
 
 
+def _scratch(name, t, device):
+    """The address of caller-supplied scratch memory, every byte of which the call may write."""
+    import torch
+    assert t.dtype == torch.uint8 and t.device == device and t.is_contiguous(), name
+    return t.data_ptr()
+
+
 def _empty_i8_rows(T: int, n: int, device):
     """int8 [T x n] with rows 16 bytes aligned, as the matrix-core kernels read them."""
     import torch
@@ -806,8 +813,8 @@ def vnm_spmm_i8(Q, scale, c: CompressedI8, bias=None, N: int = 2, out_dtype=None
     status = (_LIB or load_library()).vnm_spmm_i8(
         Q.data_ptr(), T, ldq, _vector("scale", scale, T, dev, torch.float32), c.values.data_ptr(), c.meta.data_ptr(),
         c.colidx.data_ptr(), 0 if packed is None else packed.data_ptr(), c.scale.data_ptr(), out, inn, c.V, N, c.M,
-        _vector("bias", bias, out, dev, torch.float16), Y.data_ptr(), ldy, _dtype_code(Y.dtype), path, _ptr(workspace),
-        0 if workspace is None else workspace.numel(), _raw_stream(dev))
+        _vector("bias", bias, out, dev, torch.float16), Y.data_ptr(), ldy, _dtype_code(Y.dtype), path,
+        0 if workspace is None else _scratch("workspace", workspace, dev), 0 if workspace is None else workspace.numel(), _raw_stream(dev))
     if status:
         _check(status, "vnm_spmm_i8")
     return Y
@@ -827,7 +834,7 @@ def vnm_stage_q(Q, M: int, staged=None):
     _check(load_library().vnm_stage_q_bytes(T, inn, M, ctypes.byref(b)), "vnm_stage_q_bytes")
     if staged is None:
         staged = torch.empty(max(b.value, 1), dtype=torch.uint8, device=dev)
-    _launch("vnm_stage_q", load_library().vnm_stage_q, dev, Q.data_ptr(), T, ldq, inn, M, staged.data_ptr(), staged.numel())
+    _launch("vnm_stage_q", load_library().vnm_stage_q, dev, Q.data_ptr(), T, ldq, inn, M, _scratch("staged", staged, dev), staged.numel())
     return staged
 
 
@@ -835,11 +842,11 @@ def vnm_spmm_i8_staged(staged, scale, c: CompressedI8, bias=None, N: int = 2, ou
     """vnm_spmm_i8 on activations staged by vnm_stage_q; `scale` fp32 [T] as there."""
     import torch
     dev, T = staged.device, scale.shape[0]
-    assert staged.is_cuda and staged.dtype == torch.uint8 and staged.is_contiguous() and c.packed is not None and c.packed.device == dev
+    assert staged.is_cuda and c.packed is not None and c.packed.device == dev
     if Y is None:
         Y = torch.empty((T, c.out), dtype=out_dtype or torch.float16, device=dev)
     ldy = _rows("Y", Y, T, c.out, dev)
-    _launch("vnm_spmm_i8_staged", load_library().vnm_spmm_i8_staged, dev, staged.data_ptr(), staged.numel(), T,
+    _launch("vnm_spmm_i8_staged", load_library().vnm_spmm_i8_staged, dev, _scratch("staged", staged, dev), staged.numel(), T,
             _vector("scale", scale, T, dev, torch.float32), c.packed.data_ptr(), c.scale.data_ptr(), c.out, c.inn, c.V, N, c.M,
             _vector("bias", bias, c.out, dev, torch.float16), Y.data_ptr(), ldy, _dtype_code(Y.dtype))
     return Y
@@ -950,8 +957,8 @@ def vnm_residual_norm_backward(h, stats, dx=None, dh=None, y=None, gate=None, ga
         _ptr(dx), _ptr(dh), h.data_ptr(), _ptr(y), _ptr(gate), _vector("post_weight", post_weight, n, dev, xt),
         _vector("post_bias", post_bias, n, dev, xt), _vector("pre_weight", pre_weight, n, dev, xt), _ptr(stats), lddx, lddho, ldh, ldy,
         ldg, _ptr(gh), _ptr(gy), _ptr(g_ow), _ptr(g_ob), _ptr(g_pw), _ptr(g_pb), _ptr(g_gate), n, n)
-    _launch("vnm_residual_norm_backward", lib.vnm_residual_norm_backward, dev, a, _ptr(workspace),
-            0 if workspace is None else workspace.numel())
+    _launch("vnm_residual_norm_backward", lib.vnm_residual_norm_backward, dev, a,
+            0 if workspace is None else _scratch("workspace", workspace, dev), 0 if workspace is None else workspace.numel())
     return ResidualNormGrads(gh, gy, g_gate, g_ow, g_ob, g_pw, g_pb)
 
 

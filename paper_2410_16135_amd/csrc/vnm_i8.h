@@ -39,8 +39,9 @@ inline I8Layout i8_layout(const Dims& d) {
   l.total = l.psel_off + up(rs * 32 * nt * i8_selectors(d.M)) + kI8Slack;
   return l;
 }
-// Staged activations: an image per (tile of kTokTile tokens, K step), 16 M rows [raw column][token] 160 bytes apart -- 8 rows that
-// differ modulo 8 then lie in 8 different eighths of the LDS banks --, padded to a multiple of 1 KiB.
+// Staged activations: an image per (tile of kTokTile tokens, K step), 16 M rows [raw column][token], padded to a multiple of 1 KiB.
+// Rows lie 144 bytes apart, 16 more than they hold: a transposing read takes 16 bytes of each of its rows, and rows that differ
+// modulo 16 then start in different banks (160 bytes, modulo 8: 1 to 4 % slower, and an eighth more to copy).
 constexpr int kImagePitchI8 = kTokTile + 16;
 inline int64_t i8_image_bytes(int M) { return ((int64_t)16 * M * kImagePitchI8 + 1023) / 1024 * 1024; }
 int64_t staged_q_bytes(int64_t T, const Dims& d);

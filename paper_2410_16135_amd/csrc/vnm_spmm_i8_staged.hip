@@ -9,7 +9,7 @@
 // vector instruction touches it.  A wave owns a block of 64 rows x 128 tokens (128 accumulators); its weights come straight
 // from the packed copy, 16 bytes per lane and tile.
 //
-// Per step a wave issues 8 matrix instructions of 32 cycles, 16 transposing reads (512 bytes each), 3 to 10 image copies and 4
+// Per step a wave issues 8 matrix instructions of 32 cycles, 16 transposing reads (512 bytes each), 2 to 9 image copies and 4
 // loads of weights; of a compute unit with 8 such waves that is 512 cycles of its matrix cores, 512 of LDS and 480 of the
 // 64 bytes per cycle that reach it (M = 5): balanced, so the loop is written in assembly with explicit waits, in which
 // younger requests stay in flight (compiled code drains all of them at each use).
@@ -129,8 +129,6 @@ int launch_stage_q(const void* Q, int64_t T, int64_t ldq, const Dims& d, void* s
 #define VNM_I8_C4_8B VNM_I8_C4_7B VNM_I8_COPY(28672)
 #define VNM_I8_C4_9A VNM_I8_C4_7A VNM_I8_COPY(16384)
 #define VNM_I8_C4_9B VNM_I8_COPY(20480) VNM_I8_COPY(24576) VNM_I8_COPY(28672) VNM_I8_COPY(32768)
-#define VNM_I8_C4_10A VNM_I8_C4_9A
-#define VNM_I8_C4_10B VNM_I8_C4_9B VNM_I8_COPY(36864)
 #define VNM_I8_C8_2A VNM_I8_COPY(0)
 #define VNM_I8_C8_2B VNM_I8_COPY(8192)
 #define VNM_I8_C8_3A VNM_I8_COPY(0) VNM_I8_COPY(8192)
@@ -372,7 +370,7 @@ spmm_i8_staged_kernel(const I8StagedArgs a) {
       if constexpr (DUAL) VNM_I8_LOOP_2(VNM_I8_C##W##_##N##A, VNM_I8_C##W##_##N##B);                \
       else VNM_I8_LOOP_1(VNM_I8_C##W##_##N##A, VNM_I8_C##W##_##N##B);                               \
     }
-    VNM_I8_GO(4, 3) VNM_I8_GO(4, 4) VNM_I8_GO(4, 5) VNM_I8_GO(4, 6) VNM_I8_GO(4, 7) VNM_I8_GO(4, 8) VNM_I8_GO(4, 9) VNM_I8_GO(4, 10)
+    VNM_I8_GO(4, 3) VNM_I8_GO(4, 4) VNM_I8_GO(4, 5) VNM_I8_GO(4, 6) VNM_I8_GO(4, 7) VNM_I8_GO(4, 8) VNM_I8_GO(4, 9)
     VNM_I8_GO(8, 2) VNM_I8_GO(8, 3) VNM_I8_GO(8, 4) VNM_I8_GO(8, 5)
 #undef VNM_I8_GO
   }

@@ -214,6 +214,23 @@ def test_product_on_streams_and_in_a_graph(T):
         assert same(eager, want) and all(same(y, want) for _, y in graphs)
 
 
+def test_scratch_memory_elsewhere_is_refused():
+    """Memory on the host, with gaps, or of another type never reaches a kernel, however large it is."""
+    c, _, _, _, _, _, Q, SX = make(256, 512, 64, 8, 700, 11)
+    need = 1 << 24
+    w = torch.ones(512, dtype=torch.float16, device=DEV)
+    for bad in (torch.empty(need, dtype=torch.uint8), torch.empty(1, dtype=torch.uint8, device=DEV).expand(need),
+                torch.empty(need // 4, dtype=torch.float32, device=DEV)):
+        with pytest.raises(AssertionError):
+            vnm.vnm_spmm_i8(Q, SX, c, workspace=bad)
+        with pytest.raises(AssertionError):
+            vnm.vnm_stage_q(Q, 8, staged=bad)
+        with pytest.raises(AssertionError):
+            vnm.vnm_spmm_i8_staged(bad, SX, c)
+        with pytest.raises(AssertionError):
+            vnm.vnm_residual_norm_backward(Q.half(), torch.zeros(700, 4, device=DEV), dx=Q.half(), pre="rms", pre_weight=w, workspace=bad)
+
+
 # --- together ---------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("T", [1, 37, 200])
