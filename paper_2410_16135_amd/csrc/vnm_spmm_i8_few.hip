@@ -1,4 +1,14 @@
 // Few tokens: the int8 product as a stream of the packed weight (vnm_spmm_i8).
+//
+// Y^T = W' . Q^T on V_SMFMAC_I32_32X32X64_I8, the compressed weight being the sparse A operand and up to 32 tokens the B operand.
+// A workgroup owns 32 or 64 rows; its waves cut K between them and add their sums through LDS at the end, which is exact in
+// int32, so any cut gives the same bits.  The kept columns of a column block are picked from a token's raw bytes by byte
+// permutations, whose selectors are laid out with the weight: activations are not re-laid, no second kernel, no workspace.
+//
+// Bound by the latency of one wave's chain (weights and activations of the next steps requested while this step's are picked),
+// then by the bytes of the packed weight (1.27 per kept value).  Weights from the last-level cache, 64:2:5 unless said:
+// 4096 x 4096 at 1 / 16 / 64 tokens 5.4 / 7.0 / 7.6 us, 11008 x 4096 8.1 / 9.1 / 15.4, 4096 x 11008 8.3 / 9.8 / 13.2,
+// 11008 x 4096 at M = 8 6.0 / 6.8 / 11.5; at one token 1.6, 2.9, 2.8 and 2.4 TB/s.
 #include "vnm_i8.h"
 #include "vnm_i8_rules.h"
 
@@ -42,6 +52,11 @@ __device__ __forceinline__ i8v i8_gather(const unsigned (&x)[2 * M], const u4v* 
   return b;
 }
 
+// K steps of a chunk of activations: the next chunk is requested when this one goes to LDS, so it has that long to arrive.  Four
+// steps for groups of four tokens, where they are a load or two per lane (4096 x 4096, M = 5: two steps 6.2 us, four 5.4; eight cost
+// short layers what they give here: 1000 x 1030, M = 7 3.0 -> 3.5).
+constexpr int i8_few_chunk(int M, int TT) { return TT == 4 && M <= 8 ? 4 : 2; }
+
 // M: columns per block.  NT: column tables per 64-row block.  AT: 32-row tiles per workgroup (a row block's, or one of them).
 // TT: tokens per workgroup.  WAVES: they cut the K steps between them, a contiguous run each.
 template <int M, int NT, int AT, int TT, int WAVES>
@@ -49,11 +64,13 @@ __global__ void __launch_bounds__(64 * WAVES)
 spmm_i8_few_kernel(const I8FewArgs a, const int tp) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int NSEL = i8_selectors(M), G = (TT + 31) / 32, TABLES = AT == 2 ? NT : 1;
-  constexpr int CS = M <= 8 ? 2 : 1;               // K steps of a chunk of activations
+  constexpr int CS = i8_few_chunk(M, TT);          // K steps of a chunk of activations
   constexpr int PIECES = CS * M;                   // its 16-byte pieces per token
   constexpr int PITCH = PIECES * 16 + (M % 2 ? 8 : 16);   // 2 or 4 times an odd number of dwords: the lanes' reads below cover all banks
   constexpr int NX = (TT * PIECES + 63) / 64;      // pieces per lane
-  constexpr int RC = 2;                            // chunks of weights that a wave requests ahead
+  // Fewer registers and with them more waves beat a longer reach from 16 tokens on: 11008 x 4096, M = 5 at 16 tokens 9.7 us with
+  // four, 9.1 with two, 4096 x 11008 10.5 and 9.8 (but 4096 x 4096, a workgroup on every other compute unit, 6.7 and 7.0)
+  constexpr int RW = TT == 4 ? 4 : 2;               // K steps whose weights are in flight
   const int lane = threadIdx.x & 63, j = lane & 31, h = lane >> 5;
   const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned n = blockIdx.x;
@@ -83,17 +100,17 @@ spmm_i8_few_kernel(const I8FewArgs a, const int tp) {
     xcol[i] = piece * 16;
     xdst[i] = tok * PITCH + piece * 16;
   }
-  u4v xr[NX];
+  u4v xr[NX];                                      // (passed to what follows: captured, it costs up to 9 % at 32 tokens)
   // A piece that begins inside the row is read whole: it is aligned, so what it holds past the row's end stands in the same
   // 16 bytes as the row's last channel.  Columns past the end meet weights that are zero.
-  auto load_x = [&](unsigned s) {
+  auto load_x = [&](u4v (&xr)[NX], unsigned s) {
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
       const unsigned c = s * (16 * M) + xcol[i];
       xr[i] = *(const u4v*)(xbase + (xrow[i] + (c < (unsigned)a.in ? c : 0u)));
     }
   };
-  auto store_x = [&]() {
+  auto store_x = [&](const u4v (&xr)[NX]) {
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
       if constexpr (M % 2 == 0) *(u4v*)(xs + xdst[i]) = xr[i];
@@ -151,29 +168,29 @@ spmm_i8_few_kernel(const I8FewArgs a, const int tp) {
       }
     }
   };
-  Slot ring[RC][CS];
-  load_x(s0);
+  constexpr int BODY = CS > RW ? CS : RW;          // steps after which chunks and slots are back in place
+  static_assert(BODY % CS == 0 && BODY % RW == 0, "whole chunks and rounds of slots");
+  Slot ring[RW];
+  load_x(xr, s0);
 #pragma unroll
-  for (int c = 0; c < RC; ++c)
+  for (int k = 0; k < RW; ++k) load_w(ring[k], s0 + k);
+  for (unsigned sb = s0; sb < s1; sb += BODY) {
 #pragma unroll
-    for (int k = 0; k < CS; ++k) load_w(ring[c][k], s0 + c * CS + k);
-  for (unsigned sb = s0; sb < s1; sb += RC * CS) {
-#pragma unroll
-    for (int c = 0; c < RC; ++c) {
-      const unsigned sc = sb + c * CS;
+    for (int c = 0; c < BODY; c += CS) {
+      const unsigned sc = sb + c;
       if (sc >= s1) break;
       // The chunk's activations go through LDS, where each lane finds the run of its token.  The region is the wave's own and
       // LDS executes a wave's accesses in order; the fences keep the compiler from moving reads and writes past each other.
       __builtin_amdgcn_wave_barrier();
-      store_x();
+      store_x(xr);
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      load_x(sc + CS);
+      load_x(xr, sc + CS);
 #pragma unroll
       for (int k = 0; k < CS; ++k) {
-        if (sc + k < s1) multiply(ring[c][k], k);
-        load_w(ring[c][k], sc + RC * CS + k);
+        if (sc + k < s1) multiply(ring[(c + k) % RW], k);
+        load_w(ring[(c + k) % RW], sc + k + RW);
       }
     }
   }
@@ -202,7 +219,7 @@ spmm_i8_few_kernel(const I8FewArgs a, const int tp) {
 
 template <int M, int NT, int AT, int TT, int WAVES>
 static int launch_few_cfg(const I8FewArgs& a, int64_t R64, hipStream_t st) {
-  constexpr int CS = M <= 8 ? 2 : 1, PITCH = CS * M * 16 + (M % 2 ? 8 : 16);
+  constexpr int CS = i8_few_chunk(M, TT), PITCH = CS * M * 16 + (M % 2 ? 8 : 16);
   auto kern = spmm_i8_few_kernel<M, NT, AT, TT, WAVES>;
   const int tp = (int)(a.T < TT ? a.T : TT) | 1;
   const size_t xs = (size_t)WAVES * TT * PITCH, sums = (size_t)WAVES * 32 * AT * tp * 4, lds = xs > sums ? xs : sums;
