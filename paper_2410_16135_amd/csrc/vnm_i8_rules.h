@@ -19,8 +19,8 @@ inline double i8_few_us(I8FewShape s, int64_t T, int64_t R64, int64_t S, int M) 
   return 2.5 + (double)((wgs + 255) / 256) * (fixed + step * (double)S);
 }
 inline I8FewShape i8_few_shape(int64_t T, int64_t R64, int64_t S, int M) {
-  // Eight waves where K is long and half of the compute units would be idle: 4096 x 11008, M = 5 at 1 / 16 tokens 8.1 / 9.8 us
-  // with eight, 9.1 / 10.8 with four; 4096 x 4096 (52 steps) 5.4 / 6.2 and 4.8 / 5.6.
+  // Eight waves where K is long and half of the compute units would be idle: 4096 x 11008, M = 5 at 1 / 16 tokens 7.6 / 9.1 us
+  // with eight, 9.1 / 10.5 with four; 4096 x 4096 (52 steps) 5.5 / 6.3 and 5.6 / 6.3.
   const int waves = S >= 96 && 2 * R64 <= 128 ? 8 : 4;
   // Groups of four tokens where all of their workgroups run at once: 176 x 5416, M = 5, 8 tokens 6.0 us, in one group of 16 6.6;
   // 144 x 2424, M = 4, 25 tokens 4.8 and 5.2

@@ -5,8 +5,8 @@
 // the tokens.  One pass over the tokens does both: a worker (the threads that share a row) owns a run of consecutive tokens of
 // one gate row, keeps its share of the column sums in registers, and leaves them at the end as one row of partial sums in the
 // workspace; a second kernel adds the workers' rows in a fixed order.  Bound by memory, and by the waves that fit beside the column
-// sums in registers: 4096 x 4096 bf16 without a post norm 45 us, with all calls of the second kernel 61; 1576 x 384 fp32 with gate
-// rows 14.
+// sums in registers: 4096 x 4096 bf16 with rms norms on both sides 52 us (3.9 TB/s) and 7 in the second kernel; 1576 x 384, fp32
+// stream, a gate per 197 tokens 11.5 and 3.9.
 #include "vnm_norm.h"
 
 namespace vnm {

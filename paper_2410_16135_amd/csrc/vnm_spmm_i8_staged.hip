@@ -16,7 +16,7 @@
 //
 // Measured: 4096 tokens x 4096 x 4096 at 64:2:5 38 us after 9.5 us of staging (3.6 P dense-equivalent operations per second), of
 // which the loop is 28.8 (0.55 per step: the matrix cores are busy for half of it, at the clock that the chip holds under them),
-// the prologue 0.7, and writing Y 6.3, when nothing else runs; 4096 x 11008 77 and 22.  At 256 tokens (64 workgroups of two wave
+// the prologue 0.7, and writing Y 6.3, when nothing else runs; 4096 x 11008 81 and 22.  At 256 tokens (64 workgroups of two wave
 // groups) 12.5 of 17.4.  Without the image copies, the weights or the LDS reads the 4096-token call takes 2.6, 1.6 and 3.8 us less
 // of 53; a ring of six images instead of four and weights six steps ahead instead of three gave nothing.
 #include <type_traits>
@@ -297,7 +297,7 @@ struct I8StagedArgs {
   const unsigned char* pa; const unsigned char* pidx; const unsigned char* pcol;
   int64_t out, R, S;
   int image;                       // bytes, a multiple of 1024
-  int wide_store, vec_store;       // 16-byte stores of 16-bit results, of fp32 results
+  int run;                         // results that a lane stores at once: 16 bytes where Y's rows are aligned to them
   I8Epilogue e;
 };
 
@@ -382,6 +382,9 @@ spmm_i8_staged_kernel(const I8StagedArgs a) {
   }
 
   constexpr int BE = BT / KG;                            // its token tiles
+  // What is derived from the lane is computed again: kept from before the loop it would leave no room beside the accumulators.
+  int le = lane;
+  asm volatile("" : "+v"(le));
   constexpr int EP = 64 * 2 + 8, EPB = TE * EP + 1024;   // bytes of LDS per token, and per wave
   unsigned char* ep = smem + (size_t)wave_id * EPB;
   if constexpr (KG == 2) {
@@ -401,7 +404,7 @@ spmm_i8_staged_kernel(const I8StagedArgs a) {
         acc[i][j] = kg ? acc[i][j + BE] : acc[i][j];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          *(i4v*)(mine + (((i * BE + j) * 4 + k) * 64 + lane) * 16) = (i4v){send[4 * k], send[4 * k + 1], send[4 * k + 2], send[4 * k + 3]};
+          *(i4v*)(mine + (((i * BE + j) * 4 + k) * 64 + le) * 16) = (i4v){send[4 * k], send[4 * k + 1], send[4 * k + 2], send[4 * k + 3]};
       }
     __syncthreads();
 #pragma unroll
@@ -410,7 +413,7 @@ spmm_i8_staged_kernel(const I8StagedArgs a) {
       for (int j = 0; j < BE; ++j)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const i4v v = *(const i4v*)(theirs + (((i * BE + j) * 4 + k) * 64 + lane) * 16);
+          const i4v v = *(const i4v*)(theirs + (((i * BE + j) * 4 + k) * 64 + le) * 16);
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[i][j][4 * k + e] += v[e];
         }
@@ -418,21 +421,20 @@ spmm_i8_staged_kernel(const I8StagedArgs a) {
     static_assert(EPB <= XB, "the turned-around tile fits there");
   }
   if (!r_valid) return;
-  const int tokl = lane & 31, hB = lane >> 5;
+  const int tokl = le & 31, hB = le >> 5;
   float* const scales = (float*)(ep + TE * EP);          // [64 channels][64 biases][TE tokens], this wave's own
-  scales[lane] = sw_lane;
-  scales[64 + lane] = bias_lane;
+  scales[le] = sw_lane;
+  scales[64 + le] = bias_lane;
 #pragma unroll
-  for (int k = 0; k < TE / 64; ++k) scales[128 + k * 64 + lane] = sx_lane[k];
+  for (int k = 0; k < TE / 64; ++k) scales[128 + k * 64 + le] = sx_lane[k];
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   float sx[BE];
 #pragma unroll
   for (int j = 0; j < BE; ++j) sx[j] = scales[128 + j * 32 + tokl];
-  const bool half = a.e.y_dtype != VNM_F32;
   // (type and bias are decided once: decided at each of the 128 values of a lane they cost a third of this part's time)
-  auto each = [&](auto has_bias, auto&& take) {
+  auto each = [&](auto has_bias, int j0, int j1, auto&& take) {
 #pragma unroll
     for (int i = 0; i < AT; ++i)
 #pragma unroll
@@ -440,7 +442,7 @@ spmm_i8_staged_kernel(const I8StagedArgs a) {
         const int row = i * 32 + 8 * jq + 4 * hB;        // of the lane's four channels
         const f4v sw = *(const f4v*)(scales + row), bias = *(const f4v*)(scales + 64 + row);
 #pragma unroll
-        for (int j = 0; j < BE; ++j) {
+        for (int j = j0; j < j1; ++j) {
           float v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = i8_result(acc[i][j][4 * jq + e], sw[e], sx[j], decltype(has_bias)::value, bias[e]);
@@ -448,46 +450,78 @@ spmm_i8_staged_kernel(const I8StagedArgs a) {
         }
       }
   };
-  auto either = [&](auto&& take) { if (a.e.bias) each(std::true_type{}, take); else each(std::false_type{}, take); };
-  if (!(half && a.wide_store)) {
-    either([&](int row, int j, const float (&v)[4]) {
-      const int64_t t = t_wave + j * 32 + tokl, o = r * 64 + row;
-      if (t >= a.T) return;
-      if (!half && a.vec_store && o + 3 < a.out)
-        __builtin_nontemporal_store((f4v){v[0], v[1], v[2], v[3]}, (f4v*)((float*)a.e.Y + t * a.e.ldy + o));
-      else {
+  auto either = [&](int j0, int j1, auto&& take) {
+    if (a.e.bias) each(std::true_type{}, j0, j1, take); else each(std::false_type{}, j0, j1, take);
+  };
+  auto turned = [&] {                                    // this wave's own region of LDS: in order, only the compiler is held
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  // Results are turned around in LDS, from 4 channels of a token per lane to whole runs of a token's row, whatever their
+  // alignment: stored from where they are, fp32 and unaligned rows took as long as the rest of the call (2122 tokens, 3496 x 208, M = 4,
+  // fp32 40.1 us, now 17.1; 1844, 5824 x 3904 86.9 and 43.7; 389, 10654 x 1584 fp16 33.9 and 20.1).  Y is not read again here: non-temporal stores keep it from displacing what others stream through L2.
+  // fp32: 32 tokens at a time, PER channels per lane
+  auto rows32 = [&](auto per_lane) {
+    constexpr int PER = decltype(per_lane)::value, P32 = 64 * 4 + 16;
+    static_assert(32 * P32 <= TE * EP, "a tile of fp32 results");
+    const int ch = le % (64 / PER) * PER, tl = le / (64 / PER);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) if (o + e < a.out) i8_store(a.e, t, o + e, v[e]);
+    for (int j = 0; j < BE; ++j) {
+      either(j, j + 1, [&](int row, int, const float (&v)[4]) { *(f4v*)(ep + tokl * P32 + row * 4) = (f4v){v[0], v[1], v[2], v[3]}; });
+      turned();
+#pragma unroll 4
+      for (int it = 0; it < 32 / PER; ++it) {
+        const int tk = it * PER + tl;
+        const int64_t t = t_wave + j * 32 + tk, o = r * 64 + ch;
+        float* const y = (float*)a.e.Y + t * a.e.ldy + o;
+        const float* const from = (const float*)(ep + tk * P32) + ch;
+        if (t < a.T && o + PER <= a.out) {
+          if constexpr (PER == 4) __builtin_nontemporal_store(*(const f4v*)from, (f4v*)y);
+          else __builtin_nontemporal_store(*from, y);
+        } else if (PER > 1 && t < a.T)
+          for (int e = 0; e < PER; ++e) if (o + e < a.out) y[e] = from[e];
       }
-    });
+      turned();
+    }
+  };
+  if (a.e.y_dtype == VNM_F32) {
+    if (a.run == 4) rows32(std::integral_constant<int, 4>{}); else rows32(std::integral_constant<int, 1>{});
     return;
   }
-  // 16-bit results are turned around in LDS, from 4 channels of a token per lane to whole runs of a token's row
   auto turn = [&](int row, int j, u2v pk) { *(u2v*)(ep + (size_t)(j * 32 + tokl) * EP + row * 2) = pk; };
   if (a.e.y_dtype == VNM_F16)
-    either([&](int row, int j, const float (&v)[4]) {
+    either(0, BE, [&](int row, int j, const float (&v)[4]) {
       typedef _Float16 h4 __attribute__((ext_vector_type(4)));
       turn(row, j, __builtin_bit_cast(u2v, (h4){(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]}));
     });
   else
-    either([&](int row, int j, const float (&v)[4]) {
+    either(0, BE, [&](int row, int j, const float (&v)[4]) {
       turn(row, j, (u2v){bf16_bits(v[0]) | (unsigned)bf16_bits(v[1]) << 16, bf16_bits(v[2]) | (unsigned)bf16_bits(v[3]) << 16});
     });
-  const int ch = lane & 7, tl = lane >> 3;
-  unsigned short* Y = (unsigned short*)a.e.Y;
-#pragma unroll
-  for (int it = 0; it < TE / 8; ++it) {
-    const int tk = it * 8 + tl;
-    const u2v v0 = *(const u2v*)(ep + (size_t)tk * EP + ch * 16), v1 = *(const u2v*)(ep + (size_t)tk * EP + ch * 16 + 8);
-    const u4v v = {v0.x, v0.y, v1.x, v1.y};
-    const int64_t t = t_wave + tk, o = r * 64 + ch * 8;
-    // (Y is not read again here: non-temporal stores keep it from displacing what other workgroups stream through L2)
-    if (t < a.T && o + 8 <= a.out) __builtin_nontemporal_store(v, (u4v*)(Y + t * a.e.ldy + o));
-    else if (t < a.T) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) if (o + e < a.out) Y[t * a.e.ldy + o + e] = (unsigned short)(v[e >> 1] >> (16 * (e & 1)));
+  turned();
+  auto rows16 = [&](auto per_lane) {
+    constexpr int PER = decltype(per_lane)::value;
+    const int ch = le % (64 / PER) * PER, tl = le / (64 / PER);
+#pragma unroll 8
+    for (int it = 0; it < TE / PER; ++it) {
+      const int tk = it * PER + tl;
+      const int64_t t = t_wave + tk, o = r * 64 + ch;
+      unsigned short* const y = (unsigned short*)a.e.Y + t * a.e.ldy + o;
+      const unsigned short* const from = (const unsigned short*)(ep + (size_t)tk * EP) + ch;
+      if (t < a.T && o + PER <= a.out) {
+        if constexpr (PER == 8) {
+          const u2v v0 = *(const u2v*)from, v1 = *(const u2v*)(from + 4);
+          __builtin_nontemporal_store((u4v){v0.x, v0.y, v1.x, v1.y}, (u4v*)y);
+        } else if constexpr (PER == 2) __builtin_nontemporal_store(*(const unsigned*)from, (unsigned*)y);
+        else __builtin_nontemporal_store(*from, y);
+      } else if (PER > 1 && t < a.T)
+        for (int e = 0; e < PER; ++e) if (o + e < a.out) y[e] = from[e];
     }
-  }
+  };
+  if (a.run == 8) rows16(std::integral_constant<int, 8>{});
+  else if (a.run == 2) rows16(std::integral_constant<int, 2>{});
+  else rows16(std::integral_constant<int, 1>{});
 }
 
 template <int WR, int KG, int NCW, int NBUF, bool DUAL>
@@ -543,10 +577,10 @@ int launch_spmm_i8_staged(const void* staged, int64_t T, const void* packed, con
   const I8Layout l = i8_layout(d);
   const unsigned char* p = (const unsigned char*)packed;
   I8StagedArgs a{(const unsigned char*)staged, T, p, p + l.pidx_off, p + l.pcol_off, d.out, packed_row_blocks(d), i8_steps(d),
-                 (int)i8_image_bytes(d.M), 0, 0, e};
-  const bool half = e.y_dtype != VNM_F32;
-  a.wide_store = half && e.ldy % 8 == 0 && ((uintptr_t)e.Y & 15) == 0;
-  a.vec_store = !half && e.ldy % 4 == 0 && ((uintptr_t)e.Y & 15) == 0;
+                 (int)i8_image_bytes(d.M), 1, e};
+  auto aligned = [&](int elements, int bytes) { return e.ldy % elements == 0 && ((uintptr_t)e.Y & (bytes - 1)) == 0; };
+  if (e.y_dtype == VNM_F32) a.run = aligned(4, 16) ? 4 : 1;
+  else a.run = aligned(8, 16) ? 8 : aligned(2, 4) ? 2 : 1;
   const int64_t tiles = (T + kTokTile - 1) / kTokTile;
   const bool dual = packed_tables(d.V) == 2;
   const bool wide = i8_staged_wide(tiles, a.R);

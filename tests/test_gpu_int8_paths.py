@@ -76,3 +76,20 @@ def test_staging_reads_no_row_past_the_last():
     want = ref.product(q, sx, dense, sw, None, "fp16")
     assert same(vnm.vnm_spmm_i8(view, SX, c), want)
     assert same(vnm.vnm_spmm_i8_staged(vnm.vnm_stage_q(view, 5), SX, c), want)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("out,inn,V,M,T", [(203, 600, 64, 4, 193), (130, 100, 32, 8, 140), (602, 64, 128, 4, 8300)])
+def test_stores_of_any_alignment(out, inn, V, M, T, dtype):
+    """Two groups of waves on halves of K, one group, and eight row blocks: rows of Y that allow stores of 16 bytes, of 4, of one
+    value; the values around Y stay."""
+    c, q, sx, sw, bias, dense, Q, SX = make(out, inn, V, M, T, out + T)
+    staged, b = vnm.vnm_stage_q(Q, M), torch.from_numpy(bias).to(DEV)
+    want = ref.product(q, sx, dense, sw, bias, dtype)
+    for first, ld in ((0, 608), (2, 608), (1, 608), (0, 606), (4, 604), (0, 605)):
+        buf = torch.full((T + 2, ld + 8), 42.0, dtype=ref.TYPES[dtype], device=DEV)
+        view = buf.as_strided((T, out), (ld, 1), ld + 3 - (ld + 3) % 8 + first)
+        vnm.vnm_spmm_i8_staged(staged, SX, c, bias=b, Y=view)
+        assert same(view, want), (first, ld)
+        view.fill_(42.0)
+        assert bool((buf == 42.0).all())
