@@ -34,7 +34,8 @@ typedef unsigned u4v __attribute__((ext_vector_type(4)));
 #define VNM_GLB(T) __attribute__((address_space(1))) T*
 
 // ---------------------------------------------------------------- staging
-// One workgroup: one token tile x KC K steps.  Bound by memory: 4096 x 4096 in 9.5 us (3.6 TB/s), 4096 x 11008 in 22 (4.2).  Rows are read 16 bytes per lane, parked in LDS as [token][column], and read back
+// One workgroup: one token tile x KC K steps.  Bound by memory: 4096 x 4096 in 9.5 us (3.6 TB/s), 4096 x 11008 in 22 (4.2).
+// Rows are read 16 bytes per lane, parked in LDS as [token][column], and read back
 // by transposing reads of 8 tokens x 16 columns, after which a lane holds 16 tokens of one column: an aligned piece of an image row.
 template <int KC>
 __global__ void __launch_bounds__(256)
@@ -459,8 +460,9 @@ spmm_i8_staged_kernel(const I8StagedArgs a) {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   };
   // Results are turned around in LDS, from 4 channels of a token per lane to whole runs of a token's row, whatever their
-  // alignment: stored from where they are, fp32 and unaligned rows took as long as the rest of the call (2122 tokens, 3496 x 208, M = 4,
-  // fp32 40.1 us, now 17.1; 1844, 5824 x 3904 86.9 and 43.7; 389, 10654 x 1584 fp16 33.9 and 20.1).  Y is not read again here: non-temporal stores keep it from displacing what others stream through L2.
+  // alignment: stored from where they are, fp32 and unaligned rows took as long as the rest of the call (2122 tokens, 3496 x 208,
+  // M = 4, fp32 40.1 us, now 17.1; 1844, 5824 x 3904 86.9 and 43.7; 389, 10654 x 1584, fp16 33.9 and 20.1).  Y is not read again
+  // here: non-temporal stores keep it from displacing what others stream through L2.
   // fp32: 32 tokens at a time, PER channels per lane
   auto rows32 = [&](auto per_lane) {
     constexpr int PER = decltype(per_lane)::value, P32 = 64 * 4 + 16;
