@@ -38,13 +38,13 @@ def _shape(rule, T, out, inn, M):
     return tuple(int(v) for v in rule(call + ".tiles", call + ".tokens", call + ".waves"))
 
 
-# (tiles, tokens, waves) of the fastest shape measured, or one within a twentieth of it; us of the others in the comments
+# (tiles, tokens, waves) of the fastest shape measured, or one within a tenth of it; us of the others in the comments
 @pytest.mark.parametrize("T,out,inn,M,shape", [
-    (1, 4096, 4096, 5, (1, 4, 4)), (16, 4096, 4096, 5, (1, 16, 4)),          # 4.8 with four waves, 5.4 with eight
-    (1, 4096, 11008, 5, (1, 4, 8)), (16, 4096, 11008, 5, (1, 16, 8)),        # 9.1 with four, 8.1; 10.8, 9.8
-    (8, 176, 5416, 5, (1, 4, 4)), (25, 144, 2424, 4, (1, 4, 4)),             # one group of 16: 6.6, 6.0; two: 5.2, 4.8
-    (64, 4096, 4096, 5, (1, 32, 4)), (128, 4096, 4096, 5, (2, 32, 4)),       # at 16 tokens 8.9, 7.3; at 32 of one tile 11.0, 8.4
-    (583, 685, 1296, 5, (2, 32, 4)), (71, 296, 1288, 8, (1, 16, 4)),         # at 16 9.4, 6.5; at 32 5.0, 4.4
+    (1, 4096, 4096, 5, (1, 4, 4)), (16, 4096, 4096, 5, (1, 16, 4)),          # four waves 5.3, eight 5.4; 6.5, 6.0
+    (1, 4096, 11008, 5, (1, 4, 8)), (16, 4096, 11008, 5, (1, 16, 8)),        # four waves 8.3, eight 7.9; 11.1, 8.9
+    (8, 176, 5416, 5, (1, 4, 4)), (25, 144, 2424, 4, (1, 4, 4)),             # one group of 16: 6.8, four 5.7; 5.0, 4.5
+    (64, 4096, 4096, 5, (1, 32, 4)), (128, 4096, 4096, 5, (2, 32, 4)),       # at 16 tokens 8.4, 8.0; at 32 of one tile 11.1, 9.0
+    (583, 685, 1296, 5, (2, 32, 4)), (71, 296, 1288, 8, (1, 16, 4)),         # at 16 7.8, 6.6; at 32 5.0, 4.3
 ])
 def test_shapes(rule, T, out, inn, M, shape):
     assert _shape(rule, T, out, inn, M) == shape
@@ -52,10 +52,10 @@ def test_shapes(rule, T, out, inn, M, shape):
 
 # few-token kernel where it was the faster one; us of it and of staging with the product
 @pytest.mark.parametrize("T,out,inn,M,few", [
-    (128, 4096, 4096, 5, 1), (256, 4096, 4096, 5, 1), (700, 4096, 4096, 5, 0),             # 8.5 / 24, 13.4 / 24.6, 34 / 27
-    (700, 4096, 11008, 5, 0), (4096, 4096, 11008, 5, 0), (700, 2304, 768, 8, 1),           # 70 / 49, - / 105, 10.7 / 14.8
-    (2048, 2304, 768, 8, 0), (916, 592, 10744, 10, 1), (1320, 1424, 129, 8, 1),            # 23.5 / 15.7, 24.8 / 47.8, 11.3 / 15.7
-    (2241, 6848, 256, 6, 0), (4847, 648, 6704, 4, 0)])                                     # 72.8 / 16.5, - / 61
+    (128, 4096, 4096, 5, 1), (256, 4096, 4096, 5, 1), (700, 4096, 4096, 5, 0),             # 9.1 / 24, 13.4 / 24.3, 29 / 27.6
+    (700, 4096, 11008, 5, 0), (4096, 4096, 11008, 5, 0), (700, 2304, 768, 8, 1),           # 64 / 49, - / 105, 10.0 / 13.5
+    (2048, 2304, 768, 8, 0), (916, 592, 10744, 10, 1), (1320, 1424, 129, 8, 1),            # 18.4 / 14.5, 24.3 / 47, 10.2 / 15.2
+    (2241, 6848, 256, 6, 0), (4847, 648, 6704, 4, 0)])                                     # 45 / 16.4, 76 / 47
 def test_few_or_staged(rule, T, out, inn, M, few):
     assert rule("i8_takes_few(%d, %d, %d, %d, %d)" % (T, -(-out // 64), inn, -(-(-(-inn // M)) // 16), M)) == [few]
 
