@@ -18,7 +18,9 @@ bounded sample of the same workload.
 from __future__ import annotations
 
 import argparse
+import contextlib
 import ctypes
+import gc
 import json
 import os
 import sys
@@ -401,6 +403,21 @@ def cpu_baseline(layers):
                                                     "so the full-size figure is higher")}
 
 
+@contextlib.contextmanager
+def no_collection():
+    """Python's garbage collector is run before and held back inside: a full collection of a fresh process takes 20 to 45 ms, as long
+    as the timed region, and fell into it or not with the number of objects that the imports had left (step 12 of 20 took 21 to 45
+    ms, every other one 1.4)."""
+    gc.collect()
+    was = gc.isenabled()
+    gc.disable()
+    try:
+        yield
+    finally:
+        if was:
+            gc.enable()
+
+
 def main():
     args = parse()
     if args.gpus != 1:
@@ -481,14 +498,18 @@ def main():
     torch.cuda.synchronize()
     records = []
     t_begin = ev(); t_end = ev()
-    wall0 = time.perf_counter()
-    t_begin.record()
-    for _ in range(args.steps):
-        run_step(records, False)
-    t_end.record()
-    torch.cuda.synchronize()
-    wall = time.perf_counter() - wall0
+    with no_collection():
+        wall0 = time.perf_counter()
+        t_begin.record()
+        for _ in range(args.steps):
+            run_step(records, False)
+        t_end.record()
+        torch.cuda.synchronize()
+        wall = time.perf_counter() - wall0
     step_ms = t_begin.elapsed_time(t_end) / args.steps
+    # the same time step by step, between the ends of the last layer's products: a stall shows as one long step, a cost in all
+    ends = [t_begin] + [e[2] for (L, e) in records[len(layers) - 1::len(layers)]]
+    each_ms = [a.elapsed_time(b) for a, b in zip(ends, ends[1:])]
     # breakdown pass (after the timed region, not part of `value`): events around every call
     records_full = []
     for _ in range(max(3, min(args.steps, 10))):
@@ -695,6 +716,7 @@ def main():
         "value": dense_equiv / step_ms / 1e9,
         "unit": "TFLOP/s dense-equivalent, whole path (prune+compress, spmm, decompress)",
         "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": step_ms,
+        "step_ms": {"min": min(each_ms), "median": med(each_ms), "max": max(each_ms), "longest": each_ms.index(max(each_ms))},
         "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
         "dtype": "f16", "data": "synthetic",
         "config": {"workload": f"{args.workload} linear layers at {L0.V}:2:{L0.M}, tokens {L0.tokens}, "
