@@ -4,6 +4,10 @@
 
 namespace vnm {
 
+// What one launch of the many-token kernels takes: 65535 workgroups in y and 2^32 threads (the product's workgroups have 512 at
+// most: tiles of 128 tokens in x, groups of 4 or 8 row blocks in y); more goes in ranges, one launch each.
+constexpr int64_t kI8GridY = 65535, kI8GridTiles = 1 << 22, kI8GridRows = 4 * kI8GridY;
+
 // A launch shape of the few-token kernel: 32-row tiles and tokens per workgroup, waves that cut K between them.
 struct I8FewShape { int tiles, tokens, waves; };
 

@@ -91,14 +91,17 @@ int64_t staged_q_bytes(int64_t T, const Dims& d) {
 
 template <int KC>
 static int launch_stage_q_cfg(const void* Q, int64_t T, int64_t ldq, const Dims& d, void* staged, hipStream_t st) {
-  const int64_t tiles = (T + kTokTile - 1) / kTokTile, subs = (i8_steps(d) + KC - 1) / KC;
-  if (tiles > 65535 || subs > 0x7FFFFFFF) return VNM_ERR_UNSUPPORTED;
+  const int64_t tiles = (T + kTokTile - 1) / kTokTile, S = i8_steps(d), subs = (S + KC - 1) / KC;
   auto kern = stage_q_kernel<KC>;
   if (int rc = allow_big_lds((const void*)kern, "hipFuncSetAttribute(stage_q)")) return rc;
-  hipLaunchKernelGGL(kern, dim3((unsigned)subs, (unsigned)tiles), dim3(256), (size_t)kTokTile * (KC * d.M * 16 + 16), st,
-                     (const unsigned char*)Q, T, ldq, (int)d.in, d.M, i8_steps(d), i8_image_bytes(d.M), (unsigned char*)staged);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) { set_hip_error(e, "stage_q_kernel"); return VNM_ERR_HIP; }
+  for (int64_t tile = 0; tile < tiles; tile += kI8GridY) {         // grid.y limit
+    const int64_t nt = tiles - tile < kI8GridY ? tiles - tile : kI8GridY, t0 = tile * kTokTile;
+    hipLaunchKernelGGL(kern, dim3((unsigned)subs, (unsigned)nt), dim3(256), (size_t)kTokTile * (KC * d.M * 16 + 16), st,
+                       (const unsigned char*)Q + t0 * ldq, T - t0, ldq, (int)d.in, d.M, S, i8_image_bytes(d.M),
+                       (unsigned char*)staged + tile * S * i8_image_bytes(d.M));
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { set_hip_error(e, "stage_q_kernel"); return VNM_ERR_HIP; }
+  }
   return VNM_OK;
 }
 int launch_stage_q(const void* Q, int64_t T, int64_t ldq, const Dims& d, void* staged, hipStream_t st) {
@@ -534,7 +537,6 @@ static int launch_staged_cfg(const I8StagedArgs& a, hipStream_t st) {
   auto kern = spmm_i8_staged_kernel<WR, KG, NCW, NBUF, DUAL>;
   if (int rc = allow_big_lds((const void*)kern, "hipFuncSetAttribute(spmm_i8_staged)")) return rc;
   const int64_t tiles = (a.T + kTokTile - 1) / kTokTile, groups = (a.R + WR - 1) / WR;
-  if (tiles > 0x7FFFFFFF || groups > 65535) return VNM_ERR_UNSUPPORTED;
   hipLaunchKernelGGL(kern, dim3((unsigned)tiles, (unsigned)groups), dim3(64 * WR * KG), lds, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) { set_hip_error(e, "spmm_i8_staged_kernel"); return VNM_ERR_HIP; }
@@ -586,7 +588,23 @@ int launch_spmm_i8_staged(const void* staged, int64_t T, const void* packed, con
   const int64_t tiles = (T + kTokTile - 1) / kTokTile;
   const bool dual = packed_tables(d.V) == 2;
   const bool wide = i8_staged_wide(tiles, a.R);
-  return dual ? launch_staged<true>(a, d.M, wide, st) : launch_staged<false>(a, d.M, wide, st);
+  const int64_t S = a.S, R = a.R, y_bytes = e.y_dtype == VNM_F32 ? 4 : 2;
+  // more tiles or row blocks than a grid has room for: one launch per range of them
+  for (int64_t tile = 0; tile < tiles; tile += kI8GridTiles)
+    for (int64_t r = 0; r < R; r += kI8GridRows) {
+      const int64_t t0 = tile * kTokTile, o0 = r * kPackedRows;
+      I8StagedArgs b = a;
+      b.staged += tile * S * a.image;
+      b.T = T - t0 < kI8GridTiles * kTokTile ? T - t0 : kI8GridTiles * kTokTile;
+      b.pa += r * S * 2048; b.pidx += r * S * 512; b.pcol += r * S * 64 * (dual ? 2 : 1);
+      b.R = R - r < kI8GridRows ? R - r : kI8GridRows;
+      b.out = d.out - o0 < kI8GridRows * kPackedRows ? d.out - o0 : kI8GridRows * kPackedRows;
+      b.e.Y = (unsigned char*)e.Y + (t0 * e.ldy + o0) * y_bytes;
+      b.e.scale_x += t0; b.e.scale_w += o0;
+      if (e.bias) b.e.bias += o0;
+      if (int rc = dual ? launch_staged<true>(b, d.M, wide, st) : launch_staged<false>(b, d.M, wide, st)) return rc;
+    }
+  return VNM_OK;
 }
 
 }  // namespace vnm
