@@ -720,7 +720,8 @@ def vnm_quantize_x(X, Q=None, scale=None):
 @dataclass
 class CompressedI8:
     """A compressed layer in 8 bits (device tensors): int8 values in the order of Compressed.values, its positions and column
-    indices, the opaque matrix-core copy, and one fp32 scale per output channel."""
+    indices, the opaque matrix-core copy, and one fp32 scale per output channel.  The products check types, sizes, layouts and
+    devices of a layer once, and again after a field has been assigned."""
     values: object
     meta: object
     colidx: object
@@ -731,12 +732,34 @@ class CompressedI8:
     V: int
     M: int
 
+    def __setattr__(self, name, value):
+        self.__dict__["checked"] = False
+        self.__dict__[name] = value
+
+
+def _i8_packed_bytes(c: CompressedI8, N: int) -> int:
+    b = ctypes.c_int64(0)
+    _check(load_library().vnm_i8_packed_bytes(c.out, c.inn, c.V, N, c.M, ctypes.byref(b)), "vnm_i8_packed_bytes")
+    return b.value
+
 
 def _i8_packed(c: CompressedI8, N: int):
     import torch
-    b = ctypes.c_int64(0)
-    _check(load_library().vnm_i8_packed_bytes(c.out, c.inn, c.V, N, c.M, ctypes.byref(b)), "vnm_i8_packed_bytes")
-    return torch.empty(b.value, dtype=torch.uint8, device=c.values.device) if b.value > 0 else None
+    n = _i8_packed_bytes(c, N)
+    return torch.empty(n, dtype=torch.uint8, device=c.values.device) if n > 0 else None
+
+
+def _check_layer_i8(c: CompressedI8, N: int):
+    """What a product reads of a layer has the types, sizes and layouts that its kernels take, on the device of its values."""
+    import torch
+    s = vnm_query_sizes(c.out, c.inn, c.V, c.M, N)
+    for name, t, dt, n in (("values", c.values, torch.int8, s.values_elems), ("meta", c.meta, torch.uint8, s.meta_bytes),
+                           ("colidx", c.colidx, torch.uint8, s.colidx_bytes), ("scale", c.scale, torch.float32, c.out)):
+        assert t.device == c.values.device and t.dtype == dt and t.is_contiguous() and t.numel() == n, name
+    if c.packed is not None:
+        assert c.packed.device == c.values.device and c.packed.dtype == torch.uint8 and c.packed.is_contiguous(), "packed"
+        assert c.packed.numel() >= _i8_packed_bytes(c, N), "packed"
+    c.__dict__["checked"] = True
 
 
 def _check_triple(values, dtype, c, N):
@@ -797,6 +820,8 @@ def vnm_spmm_i8(Q, scale, c: CompressedI8, bias=None, N: int = 2, out_dtype=None
         with torch.cuda.device(dev):
             return vnm_spmm_i8(Q, scale, c, bias, N, out_dtype, path, Y, workspace)
     T, inn = Q.shape
+    if not c.checked:
+        _check_layer_i8(c, N)
     out, packed = c.out, c.packed
     assert inn == c.inn and c.values.device == dev
     ldq = _rows("Q", Q, T, inn, dev, torch.int8)
@@ -842,7 +867,9 @@ def vnm_spmm_i8_staged(staged, scale, c: CompressedI8, bias=None, N: int = 2, ou
     """vnm_spmm_i8 on activations staged by vnm_stage_q; `scale` fp32 [T] as there."""
     import torch
     dev, T = staged.device, scale.shape[0]
-    assert staged.is_cuda and c.packed is not None and c.packed.device == dev
+    if not c.checked:
+        _check_layer_i8(c, N)
+    assert staged.is_cuda and c.packed is not None and c.values.device == dev
     if Y is None:
         Y = torch.empty((T, c.out), dtype=out_dtype or torch.float16, device=dev)
     ldy = _rows("Y", Y, T, c.out, dev)
