@@ -749,6 +749,11 @@ def _i8_packed(c: CompressedI8, N: int):
     return torch.empty(n, dtype=torch.uint8, device=c.values.device) if n > 0 else None
 
 
+def _check_packed_i8(c: CompressedI8, nbytes: int):
+    _scratch("packed", c.packed, c.values.device)
+    assert c.packed.numel() >= nbytes, "packed"
+
+
 def _check_layer_i8(c: CompressedI8, N: int):
     """What a product reads of a layer has the types, sizes and layouts that its kernels take, on the device of its values."""
     import torch
@@ -757,8 +762,7 @@ def _check_layer_i8(c: CompressedI8, N: int):
                            ("colidx", c.colidx, torch.uint8, s.colidx_bytes), ("scale", c.scale, torch.float32, c.out)):
         assert t.device == c.values.device and t.dtype == dt and t.is_contiguous() and t.numel() == n, name
     if c.packed is not None:
-        assert c.packed.device == c.values.device and c.packed.dtype == torch.uint8 and c.packed.is_contiguous(), "packed"
-        assert c.packed.numel() >= _i8_packed_bytes(c, N), "packed"
+        _check_packed_i8(c, _i8_packed_bytes(c, N))
     c.__dict__["checked"] = True
 
 
@@ -788,11 +792,12 @@ def vnm_pack_i8(c: CompressedI8, N: int = 2) -> CompressedI8:
     """Fills c.packed from the triple (allocated where it is None and this V, M has one)."""
     import torch
     _check_triple(c.values, torch.int8, c, N)
-    fresh = _i8_packed(c, N)
     if c.packed is None:
-        c.packed = fresh
+        c.packed = _i8_packed(c, N)
     if c.packed is not None:
-        assert fresh is not None and c.packed.device == c.values.device and c.packed.numel() >= fresh.numel(), "packed"
+        n = _i8_packed_bytes(c, N)
+        assert n > 0, "packed"
+        _check_packed_i8(c, n)
         _launch("vnm_pack_i8", load_library().vnm_pack_i8, c.values.device, _ptr(c.values), _ptr(c.meta), _ptr(c.colidx), c.out,
                 c.inn, c.V, N, c.M, _ptr(c.packed))
     return c

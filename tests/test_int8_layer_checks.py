@@ -67,3 +67,37 @@ def test_the_products_refuse_it(name, wrong):
     for call in (lambda: vnm.vnm_spmm_i8(q, s, c), lambda: vnm.vnm_spmm_i8_staged(staged, s, c)):
         with pytest.raises(AssertionError):
             call()
+
+
+PACKED = [lambda t: t[:-1], lambda t: t[:1].expand(t.numel()), lambda t: t.float(), lambda t: t.view(torch.int8), lambda t: t.repeat(2)[::2]]
+
+
+@pytest.mark.parametrize("wrong", PACKED)
+def test_packing_refuses_other_memory(wrong, monkeypatch):
+    """Memory that is not whole bytes one after the other is not packed into, however many elements it has; nothing is allocated
+    to find out."""
+    launched = []
+    monkeypatch.setattr(binding, "_check_triple", lambda *a: None)
+    monkeypatch.setattr(binding, "_launch", lambda *a: launched.append(a))
+    monkeypatch.setattr(binding, "_i8_packed", lambda *a: pytest.fail("memory for a layer that has some"))
+    c = layer()
+    vnm.vnm_pack_i8(c)
+    assert len(launched) == 1
+    c.packed = wrong(c.packed)
+    with pytest.raises(AssertionError):
+        vnm.vnm_pack_i8(c)
+    assert len(launched) == 1
+
+
+@pytest.mark.gpu
+def test_packing_on_the_device():
+    c = layer("cuda:0")
+    for wrong in PACKED + [lambda t: t.cpu()]:
+        d = copy.copy(c)
+        d.packed = wrong(c.packed)
+        with pytest.raises(AssertionError):
+            vnm.vnm_pack_i8(d)
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    vnm.vnm_pack_i8(c)
+    assert torch.cuda.max_memory_allocated() == before
