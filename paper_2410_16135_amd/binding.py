@@ -814,6 +814,9 @@ def vnm_spmm_i8_workspace_bytes(T: int, c: CompressedI8, N: int = 2) -> int:
     return _spmm_i8_workspace_bytes(T, c.out, c.inn, c.V, N, c.M)
 
 
+_I8_MAX_ROW_PITCH = 1 << 24                          # of activations that the matrix-core kernels read
+
+
 def vnm_spmm_i8(Q, scale, c: CompressedI8, bias=None, N: int = 2, out_dtype=None, path: int = PATH_AUTO, Y=None, workspace=None):
     """Y [T x out] = (Q . Wq^T) * c.scale[o] * scale[t] + bias[o], sums exact in int32, Y in fp16, bf16 or fp32 (default fp16).
     Q, scale as vnm_quantize_x leaves them; `bias` fp16 [out].  `workspace`: optional uint8 CUDA tensor of at least
@@ -836,12 +839,13 @@ def vnm_spmm_i8(Q, scale, c: CompressedI8, bias=None, N: int = 2, out_dtype=None
         Y, ldy = torch.empty((T, out), dtype=out_dtype or torch.float16, device=dev), out
     else:
         ldy = _rows("Y", Y, T, out, dev)
+    at = Q.data_ptr()
     if workspace is None and packed is not None and path != PATH_GENERIC:
         need = _spmm_i8_workspace_bytes(T, out, inn, c.V, N, c.M)
-        if need:
+        if need and at % 16 == 0 and ldq % 16 == 0 and ldq <= _I8_MAX_ROW_PITCH:    # (else the kernel on the triple serves the call)
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     status = (_LIB or load_library()).vnm_spmm_i8(
-        Q.data_ptr(), T, ldq, _vector("scale", scale, T, dev, torch.float32), c.values.data_ptr(), c.meta.data_ptr(),
+        at, T, ldq, _vector("scale", scale, T, dev, torch.float32), c.values.data_ptr(), c.meta.data_ptr(),
         c.colidx.data_ptr(), 0 if packed is None else packed.data_ptr(), c.scale.data_ptr(), out, inn, c.V, N, c.M,
         _vector("bias", bias, out, dev, torch.float16), Y.data_ptr(), ldy, _dtype_code(Y.dtype), path,
         0 if workspace is None else _scratch("workspace", workspace, dev), 0 if workspace is None else workspace.numel(), _raw_stream(dev))
