@@ -206,15 +206,16 @@ template <typename HT, typename XT, int TPR, int NCH>
 static int launch_norm_cfg(const vnm_residual_norm_args& a, bool vec, hipStream_t st) {
   constexpr int RPB = TPR == 64 ? 4 : 1, THREADS = TPR == 64 ? 256 : TPR;
   int64_t blocks = (a.T + RPB - 1) / RPB;
-  const int64_t most = 256 * (16 * 64 / THREADS);         // 16 waves per compute unit, as many as their registers allow
+  const int64_t most = 256 * (16 * 64 / THREADS);         // 16 waves per compute unit: what the registers of all-fp32 rows allow
   if (blocks > most) blocks = most;
   hipLaunchKernelGGL((residual_norm_kernel<HT, XT, TPR, NCH>), dim3((unsigned)blocks), dim3(THREADS), 0, st, a, (int)vec);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) { set_hip_error(e, "residual_norm_kernel"); return VNM_ERR_HIP; }
   return VNM_OK;
 }
-// An octet per thread where a row has at most 8192 channels: with the next row requested ahead a thread needs about 100 registers
-// for each, and fewer waves per SIMD cost more than the barriers of rows that are spread over several.
+// An octet per thread where a row has at most 8192 channels: with the next row requested ahead a thread needs 75 to 105 registers
+// for each, and fewer waves per SIMD cost more than the barriers of rows that are spread over several.  (Two octets in 1024 threads
+// do not fit 128 registers: 148 to 316 bytes of scratch memory per thread.)
 template <typename HT, typename XT>
 static int launch_norm(const vnm_residual_norm_args& a, bool vec, hipStream_t st) {
   if (a.n <= 512) return launch_norm_cfg<HT, XT, 64, 1>(a, vec, st);

@@ -18,8 +18,11 @@ struct Cut { int64_t groups, tokens, pieces, per; };
 
 // What the call has, kBiases | kGated | kPosted; a kernel for fewer keeps fewer sums and fits more waves.
 enum { kBiases = 1, kGated = 2, kPosted = 4, kAllParts = 7 };
-// Waves per SIMD that the registers are held down for: four where that needs no scratch memory (4096 x 4096 bf16 without a post
-// norm 80 us with three, 45 with four), else three (a gate and biases at 1576 x 384: 20.7 us with four and scratch, 16.3).
+// Waves per SIMD that the registers are held down for: four, also where that takes a little scratch memory (a post norm: 12 to 28
+// bytes per thread from 2049 channels on, 56 to 88 in rows that are all fp32; 4096 x 4096 bf16 61 us with four waves, 78 with three
+// and no scratch; without a post norm, where four need none, 45 and 80); three with a gate and biases (1576 x 384: 16.3 us, with
+// four and scratch 20.7); two with everything.  1024 threads are four waves per SIMD whatever that takes: up to 176 bytes, and 684 to
+// 864 above 8192 channels.
 constexpr int back_waves(int TPR, int NCH, int PARTS) {
   return TPR == 1024 ? 4 : NCH > 1 || PARTS == kAllParts ? 2 : (PARTS & kGated) || (TPR == 64 && PARTS) ? 3 : 4;
 }
@@ -29,7 +32,8 @@ static Cut make_cut(int64_t T, int64_t n, int64_t gate_tokens, bool four_waves) 
   c.tokens = gate_tokens > 0 && gate_tokens < T ? gate_tokens : T > 0 ? T : 1;
   c.groups = T > 0 ? (T + c.tokens - 1) / c.tokens : 0;
   // Few tokens: up to 256 workers.  Many: as many as run at once with four or three waves per SIMD (one more than that and the
-  // call takes two rounds: 12608 x 768 with a gate 61 us in 1802 workers), as every one leaves a row of partial sums.
+  // call takes two rounds: 12608 x 768 with a gate 61 us in 1802 workers), as every one leaves a row of partial sums.  Up to 512
+  // channels, where a worker is one wave, half of that: 12608 x 384 and 16384 x 512 take the same time with 8 and 16 per unit.
   const int64_t per_cu = n <= 512 ? 8 : n <= 1024 ? (four_waves ? 8 : 6) : n <= 2048 ? (four_waves ? 4 : 3) : n <= 4096 ? (four_waves ? 2 : 1) : 1;
   const int64_t workers = T <= 1024 ? 256 : 256 * per_cu;
   c.per = (T + workers - 1) / workers;
