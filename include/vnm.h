@@ -414,15 +414,20 @@ int vnm_pack_i8(const void* qvalues, const void* meta, const void* colidx, int64
  *   a[t, o] = sum_b sum_{j<2} qvalues[o, 2b+j] * Q[t, b*M + colidx[o / V, b, pos_j(o, b)]]   (int32, exact)
  *   Y[t, o] = ((float)a[t, o] * scale_w[o]) * scale_x[t] + bias[o]
  * in fp32 with every operation rounded by itself, then rounded to y_dtype; all kernels give the same bits.
- * Q counts as 0 at padded columns and is never read there.
+ * Q counts as 0 at columns >= in, whatever stands there.
  *   Q        dev int8 [T x in], leading dimension ldq >= in; scale_x dev fp32 [T]; scale_w dev fp32 [out]
  *   bias     dev fp16 [out] or NULL
  *   Y        dev [T x out] of type y_dtype (a vnm_dtype), leading dimension ldy >= out
  *   packed   dev, 256-byte aligned, or NULL (the kernel on the triple then serves the call)
  *   path     a vnm_spmm_path; VNM_PATH_SMFMAC fails with UNSUPPORTED where the matrix-core kernels do not apply
  *   workspace  dev, 256-byte aligned, vnm_spmm_i8_workspace_bytes(T, ...) bytes; contents are scratch
- * The matrix-core kernels need V in {32, 64, 128}, M <= 16, ldq % 16 == 0 and Q 16-byte aligned (`in` is
- * free).  Where they apply and the workspace is missing or too small the call fails with VNM_ERR_WORKSPACE.
+ * The matrix-core kernels need V in {32, 64, 128}, M <= 16, ldq % 16 == 0, ldq <= 2^24 and Q 16-byte aligned
+ * (`in` is free).  They read a row in aligned pieces of 16 bytes and the last one whole: up to 15 bytes behind
+ * the row's end, the last row's too, have to be readable (an allocation of whole 16 bytes, as vnm_quantize_x's
+ * binding makes it, has them) and change nothing.  Where they apply and the workspace is missing or too small
+ * the call fails with VNM_ERR_WORKSPACE.  Everything else is served by the kernel on the triple, one thread
+ * per result, which reads no byte outside the rows and is slow on many tokens (4096 tokens, 4096 x 4096 from
+ * rows of 4097 bytes: 153 ms, aligned 0.05).
  * Layers whose sums could leave 32 bits (2 * col_blocks * 2^14 > 2^31 - 1) fail with VNM_ERR_UNSUPPORTED.
  * T == 0 is a successful no-op (Q, scale_x and Y may then be NULL).
  */
@@ -439,8 +444,8 @@ int vnm_spmm_i8_workspace_bytes(int64_t T, int64_t out, int64_t in, int V, int N
  *   staged   dev, 256-byte aligned, vnm_stage_q_bytes(T, in, M) bytes; depends on T, in and M only.  That
  *            size includes images that the product's look-ahead reads (and never uses), and a smaller
  *            buffer is refused (VNM_ERR_WORKSPACE)
- *   Q        as for the matrix-core kernels of vnm_spmm_i8 (ldq % 16 == 0, 16-byte aligned, M <= 16);
- *            otherwise VNM_ERR_UNSUPPORTED
+ *   Q        as for the matrix-core kernels of vnm_spmm_i8 (ldq % 16 == 0, 16-byte aligned, M <= 16, rows
+ *            read in whole pieces of 16 bytes; ldq is free here, `in` < 2^31); otherwise VNM_ERR_UNSUPPORTED
  */
 int vnm_stage_q_bytes(int64_t T, int64_t in, int M, int64_t* bytes);
 int vnm_stage_q(const void* Q, int64_t T, int64_t ldq, int64_t in, int M, void* staged, int64_t staged_bytes, void* stream);

@@ -819,7 +819,8 @@ _I8_MAX_ROW_PITCH = 1 << 24                          # of activations that the m
 
 def vnm_spmm_i8(Q, scale, c: CompressedI8, bias=None, N: int = 2, out_dtype=None, path: int = PATH_AUTO, Y=None, workspace=None):
     """Y [T x out] = (Q . Wq^T) * c.scale[o] * scale[t] + bias[o], sums exact in int32, Y in fp16, bf16 or fp32 (default fp16).
-    Q, scale as vnm_quantize_x leaves them; `bias` fp16 [out].  `workspace`: optional uint8 CUDA tensor of at least
+    Q, scale as vnm_quantize_x leaves them, `bias` fp16 [out].  Rows of Q that are not 16-byte aligned, and layers without a packed
+    copy (V = 16, M > 16), are served by a kernel that is slow on many tokens.  `workspace`: optional uint8 CUDA tensor of at least
     vnm_spmm_i8_workspace_bytes(T, c) bytes; by default the call takes one from torch's allocator."""
     import torch
     assert Q.is_cuda and Q.dim() == 2
