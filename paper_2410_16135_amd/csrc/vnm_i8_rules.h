@@ -15,7 +15,7 @@ struct I8FewShape { int tiles, tokens, waves; };
 // (first loads, sums over the waves, stores) and a part per K step, set by the loads that a wave issues (weights: 4 or 5 per
 // step; activations: tokens x M / 64) and the byte permutations (two per block for M > 8).  Fitted to 4096 x 4096 at M = 5 and 16,
 // 11008 x 4096 and 2304 x 768 at M = 8, 1 to 2048 tokens, four waves; estimated / measured: 4096 x 4096, M = 5, 16 tokens
-// 5.6 / 6.5, 512 tokens at 16 per workgroup 51 / 44, at 32 35 / 31, at 32 on two tiles 23.5 / 21.5.  Over 60 random products
+// 5.5 / 7.0, 512 tokens at 16 per workgroup 50 / 45, at 32 34 / 31, at 32 on two tiles 23.3 / 20.6.  Over 60 random products
 // the choice costs 4 % against the fastest of all shapes in the mean.
 inline double i8_few_us(I8FewShape s, int64_t T, int64_t R64, int64_t S, int M) {
   const double fixed = s.tiles == 2 ? 1.5 : s.tokens == 32 ? 1.2 : 0.9;
@@ -24,11 +24,11 @@ inline double i8_few_us(I8FewShape s, int64_t T, int64_t R64, int64_t S, int M) 
   return 2.5 + (double)((wgs + 255) / 256) * (fixed + step * (double)S);
 }
 inline I8FewShape i8_few_shape(int64_t T, int64_t R64, int64_t S, int M) {
-  // Eight waves where K is long and half of the compute units would be idle: 4096 x 11008, M = 5 at 1 / 16 tokens 7.6 / 9.1 us
-  // with eight, 9.1 / 10.5 with four; 4096 x 4096 (52 steps) 5.4 / 6.0 and 5.3 / 6.5.
+  // Eight waves where K is long and half of the compute units would be idle: 4096 x 11008, M = 5 at 1 / 16 tokens 7.6 / 9.0 us
+  // with eight, 8.6 / 12.4 with four; 4096 x 4096 (52 steps), which keeps four, 5.2 / 5.9 and 5.4 / 7.0.
   const int waves = S >= 96 && 2 * R64 <= 128 ? 8 : 4;
-  // Groups of four tokens where all of their workgroups run at once: 176 x 5416, M = 5, 8 tokens 5.7 us, in one group of 16 6.8;
-  // 144 x 2424, M = 4, 25 tokens 4.5 and 5.0
+  // Groups of four tokens where all of their workgroups run at once: 176 x 5416, M = 5, 8 tokens 5.6 us, in one group of 16 6.3;
+  // 144 x 2424, M = 4, 25 tokens 4.7 and 4.8
   if (T <= 4 || (T <= 32 && 2 * R64 * ((T + 3) / 4) <= 256)) return {1, 4, waves};
   if (T <= 16) return {1, 16, waves};
   I8FewShape best = {1, 16, waves};
@@ -41,7 +41,7 @@ inline I8FewShape i8_few_shape(int64_t T, int64_t R64, int64_t S, int M) {
 // Workgroups of 8 row blocks (otherwise 4, cutting K in two): where more than half of the compute units get one
 inline bool i8_staged_wide(int64_t tiles, int64_t R64) { return R64 >= 8 && tiles * ((R64 + 7) / 8) > 128; }
 // Estimated time of staging and product: launches, prologue and store; bytes staged; K steps of each round.  4096 x 4096, M = 5,
-// estimated / measured: 256 tokens 25 / 24.3, 700 26 / 27.6, 4096 47 / 46.6.
+// estimated / measured: 256 tokens 25.5 / 25.3, 700 26.4 / 27.5, 4096 46.4 / 48.2.
 inline double i8_staged_us(int64_t T, int64_t R64, int64_t in, int64_t S) {
   const int64_t tiles = (T + 127) / 128;
   const bool wide = i8_staged_wide(tiles, R64);

@@ -6,9 +6,10 @@
 // permutations, whose selectors are laid out with the weight: activations are not re-laid, no second kernel, no workspace.
 //
 // Bound by the latency of one wave's chain (weights and activations of the next steps requested while this step's are picked),
-// then by the bytes of the packed weight (1.27 per kept value).  Weights from the last-level cache, 64:2:5 unless said:
-// 4096 x 4096 at 1 / 16 / 64 tokens 5.4 / 7.0 / 7.6 us, 11008 x 4096 8.1 / 9.1 / 15.4, 4096 x 11008 8.3 / 9.8 / 13.2,
-// 11008 x 4096 at M = 8 6.0 / 6.8 / 11.5; at one token 1.6, 2.9, 2.8 and 2.4 TB/s.
+// then by the bytes of the packed weight (1.27 per kept value).  Call after call from a graph, the next weight each time out of the
+// last-level cache (so all times of this kernel here and in vnm_i8_rules.h), 64:2:5 unless said: 4096 x 4096 at 1 / 16 / 64 tokens
+// 5.4 / 7.1 / 7.6 us, 11008 x 4096 7.3 / 8.3 / 14.6, 4096 x 11008 7.4 / 8.8 / 12.3, 11008 x 4096 at M = 8 5.7 / 6.5 / 11.2; at one
+// token 1.6, 3.2, 3.1 and 2.5 TB/s.
 #include "vnm_i8.h"
 #include "vnm_i8_rules.h"
 
@@ -53,8 +54,8 @@ __device__ __forceinline__ i8v i8_gather(const unsigned (&x)[2 * M], const u4v* 
 }
 
 // K steps of a chunk of activations: the next chunk is requested when this one goes to LDS, so it has that long to arrive.  Four
-// steps for groups of four tokens, where they are a load or two per lane (4096 x 4096, M = 5: two steps 6.2 us, four 5.4; eight cost
-// short layers what they give here: 1000 x 1030, M = 7 3.0 -> 3.5).
+// steps for groups of four tokens, where they are a load or two per lane (4096 x 4096, M = 5: two steps 6.2 us, four 5.4, eight 5.3;
+// 11008 x 4096 7.5, 7.3, 7.3; but 4096 x 11008 7.8, 7.4, 7.9 and 1000 x 1030, M = 7 3.4, 3.2, 3.7).
 constexpr int i8_few_chunk(int M, int TT) { return TT == 4 && M <= 8 ? 4 : 2; }
 
 // M: columns per block.  NT: column tables per 64-row block.  AT: 32-row tiles per workgroup (a row block's, or one of them).
@@ -68,8 +69,8 @@ spmm_i8_few_kernel(const I8FewArgs a, const int tp) {
   constexpr int PIECES = CS * M;                   // its 16-byte pieces per token
   constexpr int PITCH = PIECES * 16 + (M % 2 ? 8 : 16);   // 2 or 4 times an odd number of dwords: the lanes' reads below cover all banks
   constexpr int NX = (TT * PIECES + 63) / 64;      // pieces per lane
-  // Fewer registers and with them more waves beat a longer reach from 16 tokens on: 11008 x 4096, M = 5 at 16 tokens 9.7 us with
-  // four, 9.1 with two, 4096 x 11008 10.5 and 9.8 (but 4096 x 4096, a workgroup on every other compute unit, 6.7 and 7.0)
+  // Fewer registers and with them more waves beat a longer reach from 16 tokens on: 11008 x 4096, M = 5 at 16 tokens 8.8 us with
+  // four, 8.3 with two, 4096 x 11008 9.7 and 8.8 (but 4096 x 4096, a workgroup on every other compute unit, 6.7 and 7.1)
   constexpr int RW = TT == 4 ? 4 : 2;               // K steps whose weights are in flight
   const int lane = threadIdx.x & 63, j = lane & 31, h = lane >> 5;
   const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

@@ -14,11 +14,10 @@
 // 64 bytes per cycle that reach it (M = 5): balanced, so the loop is written in assembly with explicit waits, in which
 // younger requests stay in flight (compiled code drains all of them at each use).
 //
-// Measured: 4096 tokens x 4096 x 4096 at 64:2:5 38 us after 9.5 us of staging (3.6 P dense-equivalent operations per second), of
-// which the loop is 28.8 (0.55 per step: the matrix cores are busy for half of it, at the clock that the chip holds under them),
-// the prologue 0.7, and writing Y 6.3, when nothing else runs; 4096 x 11008 81 and 22.  At 256 tokens (64 workgroups of two wave
-// groups) 12.5 of 17.4.  Without the image copies, the weights or the LDS reads the 4096-token call takes 2.6, 1.6 and 3.8 us less
-// of 53; a ring of six images instead of four and weights six steps ahead instead of three gave nothing.
+// Measured: 4096 tokens x 4096 x 4096 at 64:2:5 40 us after 8.9 us of staging (3.4 P dense-equivalent operations per second), by time
+// stamps in a copy of the kernel 0.7 in the prologue, 0.55 per step of the loop and 6.3 for writing Y; 4096 x 11008 85 and 20.  Counters
+// of these two: the matrix cores work 33 and 39 % of the cycles in which the compute units do, LDS 37 and 40 (nearly half of that
+// for bank conflicts), so neither bounds it alone.  At 256 tokens (64 workgroups of two wave groups) 19.5 and 5.1.
 #include <type_traits>
 #include "vnm_i8.h"
 #include "vnm_i8_rules.h"
@@ -34,7 +33,7 @@ typedef unsigned u4v __attribute__((ext_vector_type(4)));
 #define VNM_GLB(T) __attribute__((address_space(1))) T*
 
 // ---------------------------------------------------------------- staging
-// One workgroup: one token tile x KC K steps.  Bound by memory: 4096 x 4096 in 9.5 us (3.6 TB/s), 4096 x 11008 in 22 (4.2).
+// One workgroup: one token tile x KC K steps.  Bound by memory: 4096 x 4096 in 8.9 us (3.8 TB/s), 4096 x 11008 in 20.3 (4.4).
 // Rows are read 16 bytes per lane, parked in LDS as [token][column], and read back
 // by transposing reads of 8 tokens x 16 columns, after which a lane holds 16 tokens of one column: an aligned piece of an image row.
 template <int KC>
@@ -464,7 +463,7 @@ spmm_i8_staged_kernel(const I8StagedArgs a) {
   };
   // Results are turned around in LDS, from 4 channels of a token per lane to whole runs of a token's row, whatever their
   // alignment: stored from where they are, fp32 and unaligned rows took as long as the rest of the call (2122 tokens, 3496 x 208,
-  // M = 4, fp32 40.1 us, now 17.1; 1844, 5824 x 3904 86.9 and 43.7; 389, 10654 x 1584, fp16 33.9 and 20.1).  Y is not read again
+  // M = 4, fp32 40.1 us, now 17.7; 1844, 5824 x 3904 86.9 and 43.2; 389, 10654 x 1584, fp16 33.9 and 22.2).  Y is not read again
   // here: non-temporal stores keep it from displacing what others stream through L2.
   // fp32: 32 tokens at a time, PER channels per lane
   auto rows32 = [&](auto per_lane) {
